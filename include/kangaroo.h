@@ -381,6 +381,75 @@ int kg_op_philox_words(uint64_t seed, uint32_t pos0, uint32_t purpose, int n, ui
  */
 int kg_op_stream_read(const void *src_dev, size_t bytes, void *work_dev, void *hip_stream);
 
+/*
+ * A key / value cache in 4 bits, beside the caches of a context (Section 1: decoding is bound by what it reads, and at long contexts
+ * that is the cache): append, attention, eviction by accumulated attention weight, and a read for tests and tools.  5 bits a number
+ * with its scales against 16 of kv_dtype 1 and 2.  Many sequences, shared key / value heads, page tables and lengths in device memory,
+ * so that a captured graph can be replayed as the sequences grow.
+ *
+ * What is stored of x, per token, key / value head and group of 32 consecutive components (x clamped to +-65504):
+ *     m = fp16(min x),  s = fp16((max x - min x) / 15) (subtraction and division in fp32),  n = clamp(rint((x - m) / s), 0, 15) with the
+ *     exact quotient and ties to even (0 where s = 0);  value = s n + m.
+ * A group with a NaN or an infinity is held as NaN (s = NaN, m = 0): rows that see the token get NaN in that head, others do not.
+ *
+ * A physical page of T = page_tokens tokens holds for each key / value head one block of 5/4 T D bytes (D = head_dim, G = D / 32), blocks
+ * of the heads one after the other:
+ *     keys    [T][q of 4][G] 32-bit words: word (q, g) = components 32 g + 8 q + 0..7, lowest nibble first
+ *     values  [T / 4][r of 16][h of D / 64][token % 4] 16-bit words: nibble i = component 16 (4 h + i) + r
+ *     fp16: key s [T / 4][G][token % 4], key m [T][G], value s [T / 4][G][token % 4], value m [T / 4][G][token % 4]
+ * Logical page i of sequence b (tokens i T ..) is physical page page_table[b][i].  An entry outside 0 .. n_pages - 1 is no page: its
+ * tokens are not written, read as zeros and are seen by no row.
+ *
+ * The rows of a call belong to sequences: rows row_start[b] .. row_start[b + 1] - 1 are the LAST tokens of sequence b, whose length
+ * len[b] counts them (an append stores row i of n at token len - n + i; in attention that row sees the tokens 0 .. len - n + i).
+ * row_start is [n_seqs + 1], non-decreasing; rows outside row_start[0] .. row_start[n_seqs] - 1 are left as they are, and so are rows at
+ * negative tokens in append and read.  A row that sees no token gets zeros from the attention.  Lengths are clamped to 0 .. max_pages T.
+ * Rolling back is a smaller length.  After an eviction len counts the kept tokens; what a key's position was is in its rotation.
+ *
+ *   dtype        of the rows: 0 float32, 1 bfloat16, 2 float16.  Rows are [heads][head_dim], `stride` elements apart.
+ *   kg_op_kv4_page_bytes   bytes of one page of one layer; 0 for sizes that are not supported (head_dim 64 or 128, page_tokens a power of
+ *                two in 16..128, 1 .. KG_KV4_MAX_HEADS heads).  page_stride may be larger, e.g. where pages hold several layers.
+ *   kg_op_kv4_append       k, v rows (keys after the rotary embedding) into the cache.
+ *   kg_op_kv4_read         k, v rows from the cache (s n + m rounded to dtype).  k and v must not overlap.
+ *   kg_op_kv4_attention    out = softmax(scale q . K) V per row and query head; n_heads is a multiple of n_kv_heads, query head j uses key /
+ *                value head j / (n_heads / n_kv_heads).  No token at max_len or beyond is looked at, and the work is cut for sequences
+ *                of that length: max_len is the largest len, or what it may grow to under a captured graph.  All sums and the softmax
+ *                are fp32.  weights_out (may be NULL) [n_seqs][n_kv_heads][max_pages T] floats: for tokens below the sequence's length,
+ *                weights_in (NULL: 0) plus the probabilities of the token summed over the call's rows and the heads that share the
+ *                cache head; other entries are left alone.  weights_in may be weights_out.  work_dev: kg_op_kv4_work_bytes bytes
+ *                (16-byte aligned), of which nothing is kept between calls.  q and out must not overlap.  Results depend on the
+ *                arguments alone, bit for bit.  Up to 16 rows x shared heads of a sequence (n_heads / n_kv_heads x rows): a row's bits do
+ *                not depend on the other rows of the call, given the same max_len, numbers of heads and n_seqs.
+ *   kg_op_kv4_evict        keeps n_keep tokens of each sequence and head: the first n_first, the last n_recent and of the others those with
+ *                the largest weights (equal: lower token first; NaN largest), in their order, copied from src into the pages of dst
+ *                (other pages than src's, which are only read; dst's len_dev is not read: the caller sets it to min(len, n_keep)).
+ *                kept [n_seqs][n_kv_heads][n_keep]: which tokens, -1 behind a sequence that is not that long (it is copied whole).
+ *                weights_out [n_seqs][n_kv_heads][dst max_pages T]: the kept tokens' weights, then zeros.
+ * Calls launch on `hip_stream`, allocate nothing and do not synchronise.  Errors: KG_EINVAL, KG_ENOSPC (work_bytes too small, n_keep more than
+ * dst's page table reaches), KG_EHIP.  n_rows = 0 is allowed.
+ */
+#define KG_KV4_MAX_HEADS 1024
+#define KG_KV4_MAX_SEQS 4096
+typedef struct kg_kv4_cache {
+    void *pool_dev;                 /* page 0 of the layer, 16-byte aligned */
+    size_t page_stride;             /* bytes from one physical page to the next: a multiple of 16, at least kg_op_kv4_page_bytes */
+    int n_pages, page_tokens, n_kv_heads, head_dim;
+    int n_seqs, max_pages;
+    const int32_t *page_table_dev;  /* [n_seqs][max_pages] */
+    const int32_t *len_dev;         /* [n_seqs] */
+} kg_kv4_cache;
+size_t kg_op_kv4_page_bytes(int head_dim, int page_tokens, int n_kv_heads);
+int kg_op_kv4_append(const kg_kv4_cache *c, int dtype, const void *k_dev, long k_stride, const void *v_dev, long v_stride,
+                     const int32_t *row_start_dev, int n_rows, void *hip_stream);
+int kg_op_kv4_read(const kg_kv4_cache *c, int dtype, void *k_dev, long k_stride, void *v_dev, long v_stride, const int32_t *row_start_dev,
+                   int n_rows, void *hip_stream);
+size_t kg_op_kv4_work_bytes(const kg_kv4_cache *c, int n_rows, int n_heads, int max_len);
+int kg_op_kv4_attention(const kg_kv4_cache *c, int dtype, const void *q_dev, long q_stride, int n_heads, const int32_t *row_start_dev,
+                        int n_rows, int max_len, float scale, void *out_dev, long out_stride, const float *weights_in_dev,
+                        float *weights_out_dev, void *work_dev, size_t work_bytes, void *hip_stream);
+int kg_op_kv4_evict(const kg_kv4_cache *src, const kg_kv4_cache *dst, int n_keep, int n_first, int n_recent, const float *weights_in_dev,
+                    float *weights_out_dev, int32_t *kept_dev, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

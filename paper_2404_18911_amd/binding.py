@@ -42,6 +42,12 @@ class kg_profile(ctypes.Structure):
     _fields_ = [("launches", ctypes.c_longlong * 5), ("seconds", ctypes.c_double * 5), ("bytes", ctypes.c_double * 5)]
 
 
+class kg_kv4_cache(ctypes.Structure):
+    _fields_ = [("pool_dev", ctypes.c_void_p), ("page_stride", ctypes.c_size_t)] + \
+               [(n, ctypes.c_int) for n in ("n_pages", "page_tokens", "n_kv_heads", "head_dim", "n_seqs", "max_pages")] + \
+               [("page_table_dev", ctypes.c_void_p), ("len_dev", ctypes.c_void_p)]
+
+
 # every symbol include/kangaroo.h declares
 class kg_train_params(ctypes.Structure):
     _fields_ = [(n, ctypes.c_float) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")]
@@ -54,7 +60,8 @@ SYMBOLS = ["kg_stats_cr", "kg_stats_ctar", "kg_create", "kg_workspace_bytes", "k
            "kg_read_logits", "kg_read_feature", "kg_read_kv", "kg_get_state", "kg_set_profiling", "kg_get_profile", "kg_reset", "kg_last_error",
            "kg_destroy", "kg_op_packed_bytes", "kg_op_work_bytes", "kg_op_pack", "kg_op_linear", "kg_op_linear_static", "kg_op_linear_valu", "kg_op_philox_words", "kg_op_stream_read",
            "kg_train_workspace_bytes", "kg_train_bind", "kg_train_step", "kg_train_accumulate", "kg_train_apply", "kg_train_features", "kg_train_accumulate_features",
-           "kg_train_read", "kg_op_gemm_f32", "kg_op_tile_pos"]
+           "kg_train_read", "kg_op_gemm_f32", "kg_op_tile_pos",
+           "kg_op_kv4_page_bytes", "kg_op_kv4_append", "kg_op_kv4_read", "kg_op_kv4_work_bytes", "kg_op_kv4_attention", "kg_op_kv4_evict"]
 
 _lib = None
 
@@ -117,6 +124,15 @@ def lib() -> ctypes.CDLL:
     L.kg_op_tile_pos.restype = ctypes.c_int
     L.kg_op_gemm_f32.argtypes = [vp, ctypes.c_long, ctypes.c_long, vp, ctypes.c_long, ctypes.c_long, vp, ctypes.c_long,
                                  ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, vp]
+    kp, ci, cl = ctypes.POINTER(kg_kv4_cache), ctypes.c_int, ctypes.c_long
+    L.kg_op_kv4_page_bytes.argtypes = [ci, ci, ci]
+    L.kg_op_kv4_page_bytes.restype = ctypes.c_size_t
+    L.kg_op_kv4_append.argtypes = [kp, ci, vp, cl, vp, cl, vp, ci, vp]
+    L.kg_op_kv4_read.argtypes = L.kg_op_kv4_append.argtypes
+    L.kg_op_kv4_work_bytes.argtypes = [kp, ci, ci, ci]
+    L.kg_op_kv4_work_bytes.restype = ctypes.c_size_t
+    L.kg_op_kv4_attention.argtypes = [kp, ci, vp, cl, ci, vp, ci, ci, ctypes.c_float, vp, cl, vp, vp, vp, ctypes.c_size_t, vp]
+    L.kg_op_kv4_evict.argtypes = [kp, kp, ci, ci, ci, vp, vp, vp, vp]
     _lib = L
     return L
 
@@ -459,3 +475,125 @@ def op_stream_read_GBs(n_bytes: int = 2 << 30, launches: int = 5, device: str = 
     e1.record(st)
     e1.synchronize()
     return n_bytes * launches / (e0.elapsed_time(e1) * 1e-3) / 1e9
+
+
+# ---- the 4-bit key / value cache (kg_op_kv4_*) ----------------------------------------------------
+
+class Kv4Cache:
+    """One layer's 4-bit cache: a pool of pages (uint8, [n_pages] * page_stride bytes from its first element on), the page table
+    int32 [n_seqs][max_pages] and the lengths int32 [n_seqs], all contiguous tensors of one GPU that this object keeps alive.
+    page_stride: bytes from page to page where a page holds more than this layer."""
+
+    def __init__(self, pool, page_table, lens, n_kv_heads: int, head_dim: int, page_tokens: int, page_stride: Optional[int] = None):
+        import torch
+        self._torch = torch
+        self.L = lib()
+        need = self.L.kg_op_kv4_page_bytes(head_dim, page_tokens, n_kv_heads)
+        if need == 0:
+            raise ValueError(f"no 4-bit cache of {n_kv_heads} heads of {head_dim} in pages of {page_tokens} tokens")
+        stride = need if page_stride is None else int(page_stride)
+        if stride < need or stride % 16:
+            raise ValueError(f"page_stride {stride} is not a multiple of 16 of at least {need}")
+        for t, dt, nd, name in ((pool, torch.uint8, 1, "pool"), (page_table, torch.int32, 2, "page_table"), (lens, torch.int32, 1, "lens")):
+            if t.dtype != dt or t.dim() != nd or not t.is_contiguous() or t.device != pool.device or not t.is_cuda:
+                raise ValueError(f"{name} has to be a contiguous {dt} tensor of {nd} dimensions on the pool's GPU")
+        n_seqs, max_pages = page_table.shape
+        n_pages = (pool.numel() + stride - need) // stride
+        if n_pages < 1 or n_seqs < 1 or max_pages < 1 or lens.shape[0] != n_seqs:
+            raise ValueError("the pool holds no page, the page table is empty, or lens does not fit it")
+        self.pool, self.page_table, self.lens, self.device = pool, page_table, lens, pool.device
+        self.n_seqs, self.max_pages, self.n_pages = n_seqs, max_pages, n_pages
+        self.n_kv_heads, self.head_dim, self.page_tokens, self.page_stride = n_kv_heads, head_dim, page_tokens, stride
+        self.capacity = max_pages * page_tokens
+        self.c = kg_kv4_cache(pool.data_ptr(), stride, n_pages, page_tokens, n_kv_heads, head_dim, n_seqs, max_pages,
+                              page_table.data_ptr(), lens.data_ptr())
+
+    def _call(self, name, *args):
+        """The library's call on the current stream of the cache's GPU."""
+        cuda, fn = self._torch.cuda, getattr(self.L, name)
+        stream = cuda.current_stream(self.device).cuda_stream
+        if cuda.current_device() == self.device.index:
+            rc = fn(*args, stream)
+        else:
+            with cuda.device(self.device):
+                rc = fn(*args, stream)
+        if rc != KG_OK:
+            raise KangarooError(rc, name)
+
+    def _rows(self, t, heads, name):
+        """(dtype code, address, row stride) of rows [n][heads][head_dim]."""
+        torch = self._torch
+        code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(t.dtype)
+        if code is None or t.dim() != 3 or t.shape[2] != self.head_dim or (heads and t.shape[1] != heads) or t.device != self.device:
+            raise ValueError(f"{name}: rows [n][{heads or 'heads'}][{self.head_dim}] of float32, bfloat16 or float16 on {self.device} wanted")
+        if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != self.head_dim):
+            raise ValueError(f"{name}: the heads of a row have to lie together")
+        return code, t.data_ptr(), t.stride(0)
+
+    def _starts(self, row_start):
+        if row_start.dtype != self._torch.int32 or row_start.shape != (self.n_seqs + 1,) or not row_start.is_contiguous() or row_start.device != self.device:
+            raise ValueError(f"row_start has to be an int32 tensor of {self.n_seqs + 1} entries on {self.device}")
+        return row_start.data_ptr()
+
+    def _weights(self, t, name):
+        if t is None:
+            return None
+        if t.dtype != self._torch.float32 or t.shape != (self.n_seqs, self.n_kv_heads, self.capacity) or not t.is_contiguous() or t.device != self.device:
+            raise ValueError(f"{name}: contiguous float32 [{self.n_seqs}][{self.n_kv_heads}][{self.capacity}] on {self.device} wanted")
+        return t.data_ptr()
+
+
+def op_kv4_append(cache: Kv4Cache, k, v, row_start) -> None:
+    """Stores rows k, v [n][n_kv_heads][head_dim] as the last tokens of their sequences (kg_op_kv4_append)."""
+    dt, kp, ks = cache._rows(k, cache.n_kv_heads, "k")
+    dv, vp, vs = cache._rows(v, cache.n_kv_heads, "v")
+    if dt != dv or k.shape[0] != v.shape[0]:
+        raise ValueError("k and v differ in type or number of rows")
+    cache._call("kg_op_kv4_append", cache.c, dt, kp, ks, vp, vs, cache._starts(row_start), k.shape[0])
+
+
+def op_kv4_read(cache: Kv4Cache, row_start, k, v) -> None:
+    """Fills rows k, v with what the cache holds for the last tokens of the sequences (kg_op_kv4_read)."""
+    dt, kp, ks = cache._rows(k, cache.n_kv_heads, "k")
+    dv, vp, vs = cache._rows(v, cache.n_kv_heads, "v")
+    if dt != dv or k.shape[0] != v.shape[0]:
+        raise ValueError("k and v differ in type or number of rows")
+    cache._call("kg_op_kv4_read", cache.c, dt, kp, ks, vp, vs, cache._starts(row_start), k.shape[0])
+
+
+def op_kv4_work_bytes(cache: Kv4Cache, n_rows: int, n_heads: int, max_len: int) -> int:
+    """Bytes of the workspace of op_kv4_attention for these sizes."""
+    n = cache.L.kg_op_kv4_work_bytes(cache.c, n_rows, n_heads, max_len)
+    if n == 0:
+        raise ValueError(f"no attention of {n_rows} rows with {n_heads} heads over {cache.n_kv_heads} and {max_len} tokens")
+    return n
+
+
+def op_kv4_attention(cache: Kv4Cache, q, row_start, out, max_len: int, work, scale: Optional[float] = None, weights_in=None,
+                     weights_out=None) -> None:
+    """out = attention of the rows q [n][heads][head_dim] over the cache (kg_op_kv4_attention); scale: 1 / sqrt(head_dim) by default.
+    weights_out [n_seqs][n_kv_heads][capacity] = weights_in plus each cached token's probability summed over rows and heads."""
+    dt, qp, qs = cache._rows(q, 0, "q")
+    do, op, os_ = cache._rows(out, q.shape[1], "out")
+    if dt != do or q.shape[0] != out.shape[0]:
+        raise ValueError("q and out differ in type or number of rows")
+    if work.device != cache.device or not work.is_contiguous():
+        raise ValueError(f"work has to be a contiguous tensor on {cache.device}")
+    cache._call("kg_op_kv4_attention", cache.c, dt, qp, qs, q.shape[1], cache._starts(row_start), q.shape[0], max_len,
+                cache.head_dim ** -0.5 if scale is None else scale, op, os_, cache._weights(weights_in, "weights_in"),
+                cache._weights(weights_out, "weights_out"), work.data_ptr(), work.numel() * work.element_size())
+
+
+def op_kv4_evict(src: Kv4Cache, dst: Kv4Cache, n_keep: int, n_first: int, n_recent: int, weights_in, weights_out, kept) -> None:
+    """Copies n_keep tokens of each sequence and head of src (the first n_first, the last n_recent, of the others those of the largest
+    weights) into the pages of dst (kg_op_kv4_evict); kept: int32 [n_seqs][n_kv_heads][n_keep]."""
+    if src.device != dst.device:
+        raise ValueError("src and dst are on different GPUs")
+    if kept.dtype != src._torch.int32 or kept.shape != (src.n_seqs, src.n_kv_heads, n_keep) or not kept.is_contiguous() or kept.device != src.device:
+        raise ValueError(f"kept: contiguous int32 [{src.n_seqs}][{src.n_kv_heads}][{n_keep}] on {src.device} wanted")
+    if weights_in is None or weights_out is None:
+        raise ValueError("evict needs weights_in and weights_out")
+    if src.n_seqs != dst.n_seqs or src.n_kv_heads != dst.n_kv_heads or src.head_dim != dst.head_dim:
+        raise ValueError("src and dst differ in sequences or heads")
+    src._call("kg_op_kv4_evict", src.c, dst.c, n_keep, n_first, n_recent, src._weights(weights_in, "weights_in"),
+              dst._weights(weights_out, "weights_out"), kept.data_ptr())

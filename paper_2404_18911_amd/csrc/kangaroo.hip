@@ -2,6 +2,7 @@
 // it carves the caller's arena / KV pool / scratch, launches the kernels of kernels.hip.h on the
 // caller's stream, and runs the control flow of the draft-and-verify round (Section 3, Figure 2).
 #include "kernels.hip.h"
+#include "kv4.hip.h"
 #include "prompt_plan.h"
 #include "train.hip.h"
 
@@ -2489,6 +2490,175 @@ int kg_op_stream_read(const void *src, size_t bytes, void *work, void *hip_strea
     const int grid = std::max(1, std::min(2 * cus, 1024));       // work holds 1024 words
     hipLaunchKernelGGL(stream_read_kernel, dim3(grid), dim3(512), 0, (hipStream_t)hip_stream, (const u32x4_t *)src, bytes / 16,
                        (unsigned *)work);
+    return hipGetLastError() == hipSuccess ? KG_OK : KG_EHIP;
+}
+
+// ---- the 4-bit key / value cache ----
+
+static bool kv4_cache_ok(const kg_kv4_cache *c)
+{
+    return c && c->pool_dev && ((uintptr_t)c->pool_dev & 15) == 0 && kg_op_kv4_page_bytes(c->head_dim, c->page_tokens, c->n_kv_heads) != 0 &&
+           c->page_stride % 16 == 0 && c->page_stride >= kg_op_kv4_page_bytes(c->head_dim, c->page_tokens, c->n_kv_heads) && c->n_pages >= 1 &&
+           c->n_seqs >= 1 && c->n_seqs <= KG_KV4_MAX_SEQS && c->max_pages >= 1 && c->max_pages <= (1 << 30) / c->page_tokens &&
+           c->page_table_dev && c->len_dev;
+}
+
+static Kv4View kv4_view(const kg_kv4_cache *c)
+{
+    Kv4View v;
+    v.pool = (char *)c->pool_dev; v.page_stride = c->page_stride; v.table = c->page_table_dev; v.len = c->len_dev;
+    v.n_pages = c->n_pages; v.logT = ilog2(c->page_tokens); v.H = c->n_kv_heads; v.n_seqs = c->n_seqs; v.max_pages = c->max_pages;
+    return v;
+}
+
+static size_t kv4_esz(int dtype) { return dtype == 0 ? 4 : dtype == 1 || dtype == 2 ? 2 : 0; }
+
+// rows of w elements, `stride` elements apart
+static bool kv4_rows_ok(const void *p, long stride, long w, int n_rows, size_t esz)
+{
+    return p && ((uintptr_t)p & (esz - 1)) == 0 && (n_rows <= 1 || stride >= w) && (size_t)(stride < 0 ? 0 : stride) < ((size_t)1 << 40);
+}
+
+// Do two arrays of n rows share memory?  (Two parts of one array of wider rows do not.)
+static bool kv4_rows_share(const void *a, long sa, const void *b, long sb, long w, int n, size_t esz)
+{
+    const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b, wb = (uintptr_t)w * esz;
+    const uintptr_t a1 = a0 + (uintptr_t)(n - 1) * sa * esz + wb, b1 = b0 + (uintptr_t)(n - 1) * sb * esz + wb;
+    if (a1 <= b0 || b1 <= a0) return false;
+    if (sa != sb || n == 1) return true;
+    const uintptr_t st = (uintptr_t)sa * esz, off = a0 < b0 ? (b0 - a0) % st : (a0 - b0) % st;
+    return off < wb || off + wb > st;
+}
+
+static bool bytes_share(const void *a, size_t na, const void *b, size_t nb)
+{
+    return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+
+#define KV4_BY_TYPE(launch, D)                              \
+    do {                                                    \
+        if (dtype == 0) launch(float, D);                   \
+        else if (dtype == 1) launch(__bf16, D);             \
+        else launch(_Float16, D);                           \
+    } while (0)
+#define KV4_BY_TYPE_AND_DIM(launch, dim)                    \
+    do {                                                    \
+        if ((dim) == 128) KV4_BY_TYPE(launch, 128);         \
+        else KV4_BY_TYPE(launch, 64);                       \
+    } while (0)
+
+size_t kg_op_kv4_page_bytes(int head_dim, int page_tokens, int n_kv_heads)
+{
+    if ((head_dim != 64 && head_dim != 128) || page_tokens < 16 || page_tokens > 128 || (page_tokens & (page_tokens - 1)) || n_kv_heads < 1 ||
+        n_kv_heads > KG_KV4_MAX_HEADS)
+        return 0;
+    return (size_t)n_kv_heads * page_tokens * head_dim * 5 / 4;
+}
+
+int kg_op_kv4_append(const kg_kv4_cache *c, int dtype, const void *k, long k_stride, const void *v, long v_stride, const int32_t *row_start,
+                     int n_rows, void *hip_stream)
+{
+    const size_t esz = kv4_esz(dtype);
+    if (!kv4_cache_ok(c) || !esz || n_rows < 0 || !row_start) return KG_EINVAL;
+    if (n_rows == 0) return KG_OK;
+    const long w = (long)c->n_kv_heads * c->head_dim;
+    if (!kv4_rows_ok(k, k_stride, w, n_rows, esz) || !kv4_rows_ok(v, v_stride, w, n_rows, esz)) return KG_EINVAL;
+    const Kv4View view = kv4_view(c);
+    const size_t lanes = (size_t)n_rows * c->n_kv_heads * (c->head_dim / 8);
+    if (lanes > (size_t)255 << 31) return KG_EINVAL;
+    const dim3 grid((unsigned)((lanes + 255) / 256));
+#define KV4_LAUNCH(T, D) \
+    hipLaunchKernelGGL((kv4_append_kernel<T, D>), grid, dim3(256), 0, (hipStream_t)hip_stream, view, (const T *)k, k_stride, (const T *)v, v_stride, row_start, n_rows)
+    KV4_BY_TYPE_AND_DIM(KV4_LAUNCH, c->head_dim);
+#undef KV4_LAUNCH
+    return hipGetLastError() == hipSuccess ? KG_OK : KG_EHIP;
+}
+
+int kg_op_kv4_read(const kg_kv4_cache *c, int dtype, void *k, long k_stride, void *v, long v_stride, const int32_t *row_start, int n_rows,
+                   void *hip_stream)
+{
+    const size_t esz = kv4_esz(dtype);
+    if (!kv4_cache_ok(c) || !esz || n_rows < 0 || !row_start) return KG_EINVAL;
+    if (n_rows == 0) return KG_OK;
+    const long w = (long)c->n_kv_heads * c->head_dim;
+    if (!kv4_rows_ok(k, k_stride, w, n_rows, esz) || !kv4_rows_ok(v, v_stride, w, n_rows, esz)) return KG_EINVAL;
+    if (kv4_rows_share(k, k_stride, v, v_stride, w, n_rows, esz)) return KG_EINVAL;
+    const Kv4View view = kv4_view(c);
+    const size_t lanes = (size_t)n_rows * c->n_kv_heads * (c->head_dim / 8);
+    if (lanes > (size_t)255 << 31) return KG_EINVAL;
+    const dim3 grid((unsigned)((lanes + 255) / 256));
+#define KV4_LAUNCH(T, D) \
+    hipLaunchKernelGGL((kv4_read_kernel<T, D>), grid, dim3(256), 0, (hipStream_t)hip_stream, view, (T *)k, k_stride, (T *)v, v_stride, row_start, n_rows)
+    KV4_BY_TYPE_AND_DIM(KV4_LAUNCH, c->head_dim);
+#undef KV4_LAUNCH
+    return hipGetLastError() == hipSuccess ? KG_OK : KG_EHIP;
+}
+
+static bool kv4_attn_shape_ok(const kg_kv4_cache *c, int n_rows, int n_heads, int max_len)
+{
+    return kv4_cache_ok(c) && n_rows >= 0 && n_heads >= 1 && n_heads <= KG_KV4_MAX_HEADS && n_heads % c->n_kv_heads == 0 && max_len >= 1 &&
+           max_len <= (1 << 30);
+}
+
+size_t kg_op_kv4_work_bytes(const kg_kv4_cache *c, int n_rows, int n_heads, int max_len)
+{
+    if (!kv4_attn_shape_ok(c, n_rows, n_heads, max_len)) return 0;
+    return up((size_t)n_rows * n_heads * 4) + ALIGN;
+}
+
+int kg_op_kv4_attention(const kg_kv4_cache *c, int dtype, const void *q, long q_stride, int n_heads, const int32_t *row_start, int n_rows,
+                        int max_len, float scale, void *out, long out_stride, const float *weights_in, float *weights_out, void *work,
+                        size_t work_bytes, void *hip_stream)
+{
+    const size_t esz = kv4_esz(dtype);
+    if (!kv4_attn_shape_ok(c, n_rows, n_heads, max_len) || !esz || !row_start || !std::isfinite(scale) || !work || ((uintptr_t)work & 15)) return KG_EINVAL;
+    if (weights_in && !weights_out) return KG_EINVAL;
+    if (work_bytes < kg_op_kv4_work_bytes(c, n_rows, n_heads, max_len)) return KG_ENOSPC;
+    const long w = (long)n_heads * c->head_dim;
+    if (n_rows > 0) {
+        if (!kv4_rows_ok(q, q_stride, w, n_rows, esz) || !kv4_rows_ok(out, out_stride, w, n_rows, esz)) return KG_EINVAL;
+        if (kv4_rows_share(q, q_stride, out, out_stride, w, n_rows, esz)) return KG_EINVAL;
+    }
+    const size_t cap = (size_t)c->max_pages * c->page_tokens, w_bytes = (size_t)c->n_seqs * c->n_kv_heads * cap * 4;
+    if (weights_in && weights_in != weights_out && bytes_share(weights_in, w_bytes, weights_out, w_bytes)) return KG_EINVAL;
+    if (n_rows == 0 && !weights_out) return KG_OK;
+    Kv4Attn a;
+    a.c = kv4_view(c); a.q = q; a.out = out; a.q_stride = q_stride; a.out_stride = out_stride; a.row_start = row_start; a.n_rows = n_rows;
+    a.heads = n_heads; a.max_len = (int)std::min<size_t>(max_len, cap); a.scale = scale; a.w_in = weights_in; a.w_out = weights_out; a.lse = (float *)work;
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (n_rows > 0) {
+        const dim3 grid(n_rows, n_heads);
+#define KV4_LAUNCH(T, D) hipLaunchKernelGGL((kv4_attend_kernel<T, D>), grid, dim3(128), 0, s, a)
+        KV4_BY_TYPE_AND_DIM(KV4_LAUNCH, c->head_dim);
+#undef KV4_LAUNCH
+    }
+    if (weights_out) {
+        const dim3 grid((a.max_len + 127) / 128, c->n_kv_heads, c->n_seqs);
+#define KV4_LAUNCH(T, D) hipLaunchKernelGGL((kv4_weights_kernel<T, D>), grid, dim3(128), 0, s, a)
+        KV4_BY_TYPE_AND_DIM(KV4_LAUNCH, c->head_dim);
+#undef KV4_LAUNCH
+    }
+    return hipGetLastError() == hipSuccess ? KG_OK : KG_EHIP;
+}
+
+int kg_op_kv4_evict(const kg_kv4_cache *src, const kg_kv4_cache *dst, int n_keep, int n_first, int n_recent, const float *weights_in,
+                    float *weights_out, int32_t *kept, void *hip_stream)
+{
+    if (!kv4_cache_ok(src) || !kv4_cache_ok(dst) || !weights_in || !weights_out || !kept) return KG_EINVAL;
+    if (src->head_dim != dst->head_dim || src->n_kv_heads != dst->n_kv_heads || src->n_seqs != dst->n_seqs) return KG_EINVAL;
+    if (n_keep < 1 || n_first < 0 || n_recent < 0 || n_first > n_keep || n_recent > n_keep - n_first) return KG_EINVAL;
+    const size_t in_cap = (size_t)src->max_pages * src->page_tokens, out_cap = (size_t)dst->max_pages * dst->page_tokens;
+    if ((size_t)n_keep > out_cap) return KG_ENOSPC;
+    const size_t heads = (size_t)src->n_seqs * src->n_kv_heads;
+    if (bytes_share(weights_in, heads * in_cap * 4, weights_out, heads * out_cap * 4)) return KG_EINVAL;
+    Kv4Evict a;
+    a.src = kv4_view(src); a.dst = kv4_view(dst); a.keep = n_keep; a.first = n_first; a.recent = n_recent;
+    a.w_in = weights_in; a.w_out = weights_out; a.kept = kept;
+    hipStream_t s = (hipStream_t)hip_stream;
+    hipLaunchKernelGGL(kv4_select_kernel, dim3(src->n_kv_heads, src->n_seqs), dim3(1024), 0, s, a);
+    const dim3 grid((n_keep + 63) / 64, src->n_kv_heads, src->n_seqs);
+    if (src->head_dim == 128) hipLaunchKernelGGL(kv4_move_kernel<128>, grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(kv4_move_kernel<64>, grid, dim3(256), 0, s, a);
     return hipGetLastError() == hipSuccess ? KG_OK : KG_EHIP;
 }
 

@@ -1,0 +1,628 @@
+"""The 4-bit key / value cache on the GPU against its definition in 64 bits (tests/kv4_oracle.py): append and read number by
+number, attention with the tokens' weights, eviction, and a run of them together; pages in no order, garbage in every place that
+holds no token, empty sequences, rows without tokens, missing pages, strides, graphs and streams."""
+import numpy as np
+import pytest
+
+import kv4_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+
+def _dt(name):
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[name]
+
+
+class Case:
+    """A cache on the GPU with sequences of the given capacities, pages in random order, every byte garbage (NaN scales)."""
+
+    def __init__(self, H, D, T, caps, seed=0, layers=1, spare=2, dev="cuda:0"):
+        import torch
+        from paper_2404_18911_amd import binding as B
+        self.B, self.torch, self.dev = B, torch, torch.device(dev)
+        self.H, self.D, self.T, self.caps = H, D, T, caps
+        rng = np.random.default_rng(seed)
+        need = [max(1, (c + T - 1) // T) for c in caps]
+        self.n_pages = sum(need) + spare
+        order = rng.permutation(self.n_pages)
+        self.table = np.full((len(caps), max(need)), -7, np.int32)
+        at = 0
+        for s, n in enumerate(need):
+            self.table[s, :n] = order[at:at + n]
+            at += n
+        self.block = H * T * D * 5 // 4
+        self.stride = self.block * layers
+        host = rng.integers(0, 256, self.n_pages * self.stride, dtype=np.uint8)
+        host[rng.random(len(host)) < 0.5] = 0xFF
+        self.pool = torch.from_numpy(host).to(self.dev)
+        self.lens = torch.zeros(len(caps), dtype=torch.int32, device=self.dev)
+        self.cache = B.Kv4Cache(self.pool, torch.from_numpy(self.table).to(self.dev), self.lens, H, D, T, page_stride=self.stride)
+        self.lens_host = [0] * len(caps)
+
+    def host(self):
+        return O.Pages(self.pool.cpu().numpy(), self.table, self.H, self.D, self.T, self.stride)
+
+    def set_lens(self, lens):
+        self.lens_host = list(lens)
+        self.lens.copy_(self.torch.tensor(lens, dtype=self.torch.int32))
+
+    def starts(self, rows, first=0):
+        return self.torch.tensor(np.concatenate([[0], np.cumsum(rows)]) + first, dtype=self.torch.int32, device=self.dev)
+
+    def rows(self, x, name, stride=None, shift=0):
+        """x [n][heads][D] float32 -> device rows of the type, `stride` elements apart, `shift` elements behind an aligned address;
+        what lies between is NaN."""
+        torch = self.torch
+        n, w = x.shape[0], x.shape[1] * x.shape[2]
+        stride = stride or w
+        buf = torch.full((shift + max(1, n) * stride,), float("nan"), dtype=_dt(name), device=self.dev)
+        v = torch.as_strided(buf, (n, x.shape[1], x.shape[2]), (stride, x.shape[2], 1), shift)
+        v.copy_(torch.from_numpy(x))
+        return v
+
+    def fill(self, lens, seed=1, name="f32", scale=1.0):
+        """Sequences of these lengths, appended in one call; returns their quantised keys and values per sequence."""
+        rng = np.random.default_rng(seed)
+        n = sum(lens)
+        x = [O.ROUND[name](rng.standard_normal((n, self.H, self.D)).astype(np.float32) * scale) for _ in range(2)]
+        x[0][..., rng.integers(0, self.D)] *= 6
+        x[0] = O.ROUND[name](x[0])
+        self.set_lens(lens)
+        self.B.op_kv4_append(self.cache, self.rows(x[0], name), self.rows(x[1], name), self.starts(lens))
+        q = [O.quantise(v) for v in x]
+        cut = np.cumsum([0] + list(lens))
+        return [tuple(tuple(p[a:b] for p in t) for t in q) for a, b in zip(cut[:-1], cut[1:])]
+
+    def attend(self, q, rows, name, max_len=None, scale=None, w_in=None, w_out=None, stride=None, shift=0, first=0):
+        torch, n = self.torch, q.shape[0]
+        qd = self.rows(q, name, stride, shift)
+        out = self.rows(np.full(q.shape, 777.0, np.float32), name, stride, shift)
+        max_len = max_len or max(1, max(self.lens_host))
+        work = torch.full((self.B.op_kv4_work_bytes(self.cache, n, q.shape[1], max_len),), 0xFF, dtype=torch.uint8, device=self.dev)
+        self.B.op_kv4_attention(self.cache, qd, self.starts(rows, first), out, max_len, work, scale, w_in, w_out)
+        torch.cuda.synchronize(self.dev)
+        return out.float().cpu().numpy().astype(np.float64)
+
+
+def _nibbles(pages, s, H, n):
+    out = [[], []]
+    for t in range(n):
+        per = [pages.token(s, h, t) for h in range(H)]
+        for kind in range(2):
+            out[kind].append([np.stack([p[kind][i] for p in per]) for i in range(3)])
+    return [[np.stack([t[i] for t in kind]) for i in range(3)] for kind in out]
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("H,D,T,lens,rows", [(1, 64, 16, [1], [1]), (3, 64, 32, [37, 0, 5], [37, 0, 2]), (2, 128, 16, [33], [20]), (5, 128, 64, [70, 1], [7, 1]),
+                                             (4, 128, 128, [131], [131])])
+def test_append_holds_exactly_what_the_format_says(name, H, D, T, lens, rows):
+    c = Case(H, D, T, lens, seed=3, layers=2)
+    before = c.pool.cpu().numpy().copy()
+    rng = np.random.default_rng(5)
+    n = sum(rows)
+    x = [O.ROUND[name]((rng.standard_normal((n, H, D)) * np.exp(rng.uniform(-6, 6, (n, H, 1)))).astype(np.float32)) for _ in range(2)]
+    # groups that can go wrong: constant, zero, least normal half, beyond the halves' range, borders between levels, not finite
+    x[0][0, 0, :32], x[1][0, 0, :32] = 0.37, 0.0
+    x[0][-1, -1, 32:64] = np.linspace(0, 6e-8, 32)
+    x[1][-1, -1, 32:64] = np.linspace(-3e4, 3e4, 32)
+    if name != "f16":
+        x[1][-1, 0, :32] = np.linspace(-1e5, 3e5, 32)
+    x[0][-1, 0, :32] = np.concatenate([[0, 15], np.arange(15) + 0.5, np.arange(15)])
+    x = [O.ROUND[name](v) for v in x]
+    if n > 2:
+        x[0][1, 0, 3], x[1][1, H - 1, 40], x[0][2, H - 1, 33] = np.nan, np.inf, -np.inf
+    c.set_lens(lens)
+    w = H * D
+    k, v = c.rows(x[0], name, w + 8, 8), c.rows(x[1], name, w + 3, 1)       # (the second neither aligned nor an even stride)
+    c.B.op_kv4_append(c.cache, k, v, c.starts(rows))
+    k2, v2 = c.rows(np.full_like(x[0], 5.0), "f32", w + 5, 3), c.rows(np.full_like(x[0], 5.0), "f32")
+    c.B.op_kv4_read(c.cache, c.starts(rows), k2, v2)
+    c.torch.cuda.synchronize()
+    got = [t.cpu().numpy() for t in (k2, v2)]
+    pages, q, at = c.host(), [O.quantise(t) for t in x], 0
+    touched = np.zeros(len(before), bool)
+    for s, (length, r) in enumerate(zip(lens, rows)):
+        for i in range(r):
+            t = length - r + i
+            for h in range(H):
+                tok = pages.token(s, h, t)
+                for kind in range(2):
+                    for a, b in zip(tok[kind], q[kind]):
+                        assert np.array_equal(a, b[at, h], equal_nan=True), (s, t, h, kind)
+                    want = O.values(tok[kind])
+                    ok = np.abs(got[kind][at, h] - want) <= np.abs(want) * 2.0 ** -24 + 1e-45
+                    assert (ok | (np.isnan(want) & np.isnan(got[kind][at, h]))).all()
+                touched[[int(c.table[s, t // T]) * c.stride + o for o in O.token_offsets(H, D, T, h, t % T)]] = True
+            at += 1
+    after = pages.pool
+    assert (after[~touched] == before[~touched]).all()          # nothing else in the pool changes
+
+
+@pytest.mark.parametrize("name", ["bf16", "f16"])
+def test_read_rounds_to_the_rows_type(name):
+    c = Case(2, 64, 16, [21])
+    kv = c.fill([21])[0]
+    k, v = c.rows(np.zeros((21, 2, 64), np.float32), name), c.rows(np.zeros((21, 2, 64), np.float32), name)
+    c.B.op_kv4_read(c.cache, c.starts([21]), k, v)
+    c.torch.cuda.synchronize()
+    for got, q in ((k, kv[0]), (v, kv[1])):
+        want = O.values(q)
+        assert (np.abs(got.float().cpu().numpy() - want) <= np.abs(want) * (O.HALF_STEP[name] + 2.0 ** -23)).all()
+
+
+def test_rows_that_have_no_place_are_left_alone():
+    """Rows outside the sequences, rows in front of the first token, tokens whose page does not exist."""
+    c = Case(2, 64, 16, [40, 40])
+    c.table[1, 1] = c.n_pages                                   # no page
+    c.cache.page_table.copy_(c.torch.from_numpy(c.table))
+    before = c.pool.cpu().numpy().copy()
+    rng = np.random.default_rng(0)
+    x = rng.standard_normal((60, 2, 64)).astype(np.float32)
+    c.set_lens([3, 40])
+    starts = c.torch.tensor([4, 9, 49], dtype=c.torch.int32, device=c.dev)     # 5 rows for 3 tokens; 40 rows
+    c.B.op_kv4_append(c.cache, c.rows(x, "f32"), c.rows(-x, "f32"), starts)
+    k, v = c.rows(np.full_like(x, 5.0), "f32"), c.rows(np.full_like(x, 5.0), "f32")
+    c.B.op_kv4_read(c.cache, starts, k, v)
+    c.torch.cuda.synchronize()
+    k = k.cpu().numpy()
+    q = O.values(O.quantise(x))
+    for r in range(60):
+        s, pos = (0, r - 6) if 4 <= r < 9 else (1, r - 9) if 9 <= r < 49 else (None, -1)
+        if s is None or pos < 0:
+            assert (k[r] == 5.0).all(), r
+        elif s == 1 and 16 <= pos < 32:
+            assert (k[r] == 0.0).all(), r
+        else:
+            assert np.allclose(k[r], q[r], rtol=2.0 ** -23, atol=0), r
+    changed = np.flatnonzero(c.pool.cpu().numpy() != before) // c.stride
+    assert set(changed) <= {int(c.table[0, 0]), int(c.table[1, 0]), int(c.table[1, 2])}
+
+
+def _check_attention(c, kv, q, rows, name, got, scale, max_len=None, here=None, w=None, w_in=None):
+    at = 0
+    for s, r in enumerate(rows):
+        n = c.lens_host[s]
+        pos = n - r + np.arange(r)
+        if max_len:
+            pos = np.minimum(pos, max_len - 1)
+        hs = None if here is None else here[s][:n]
+        if n == 0:
+            want = tol = np.zeros((r,) + q.shape[1:])
+            prob = np.zeros((r, q.shape[1], 0))
+        else:
+            want, tol, prob = O.attention(q[at:at + r].astype(np.float64), kv[s][0], kv[s][1], pos, scale, hs)
+        err = np.abs(got[at:at + r] - want)
+        lim = tol + O.HALF_STEP[name] * np.abs(want) + 1e-30
+        if name == "f16":
+            lim = lim + 2.0 ** -25
+        assert (err <= lim).all(), (s, float((err / lim).max()), np.argwhere(err > lim)[:4])
+        if w is not None:
+            g = q.shape[1] // c.H
+            add = prob.reshape(r, c.H, g, n).sum((0, 2))
+            base = np.zeros_like(add) if w_in is None else w_in[s][:, :n]
+            # a probability is off by twice its score's error and 2^-20 of itself; sums of r g of them and the old weight in fp32
+            rel = 2.0 ** -20 + (r * g + 2) * 2.0 ** -24
+            smax = 0.0
+            if n:
+                Ka = (np.abs(kv[s][0][0] * kv[s][0][1][..., None]) + np.abs(kv[s][0][2])[..., None]).reshape(n, c.H, c.D)
+                smax = max([float(np.max(Ka[:, j // g] @ np.abs(q[at:at + r, j].T.astype(np.float64)))) for j in range(q.shape[1])] or [0.0]) if r else 0.0
+            wt = add * (rel + 2 * smax * abs(scale) * 2.0 ** -20) + np.abs(base) * 2.0 ** -23
+            assert (np.abs(w[s][:, :n] - (base + add)) <= wt + 1e-30).all(), (s, float(np.abs(w[s][:, :n] - (base + add)).max()))
+            if max_len is None or n < max_len:
+                assert (w[s][:, n:] == -3.0).all()          # entries behind the sequence are left alone
+        at += r
+
+
+ATTN = [
+    # H, heads, D, T, lens, rows
+    (1, 1, 64, 16, [1], [1]), (2, 2, 128, 16, [15], [1]), (2, 4, 64, 16, [17], [3]), (3, 3, 128, 32, [31, 32, 33], [1, 1, 1]),
+    (1, 8, 128, 64, [129], [2]), (2, 10, 64, 128, [255, 0, 1], [7, 0, 1]), (4, 4, 128, 128, [257], [8]), (2, 2, 128, 16, [600], [1]),
+    (1, 1, 128, 32, [1030], [5]), (2, 6, 128, 16, [40], [40]), (1, 3, 64, 32, [100, 77], [33, 70]), (2, 2, 128, 128, [300], [150]),
+    (1, 16, 64, 64, [90], [20]), (3, 3, 64, 16, [5, 5, 5, 5], [5, 1, 4, 2]), (1, 32, 128, 16, [70], [1]), (1, 24, 64, 16, [64], [3]),
+]
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("H,heads,D,T,lens,rows", ATTN)
+def test_attention_and_weights(name, H, heads, D, T, lens, rows):
+    c = Case(H, D, T, [n + 20 for n in lens], seed=len(lens) + D)
+    kv = c.fill(lens, name=name)
+    rng = np.random.default_rng(7)
+    q = O.ROUND[name](rng.standard_normal((sum(rows), heads, D)).astype(np.float32) * 1.5)
+    cap = c.cache.capacity
+    w_in = rng.random((len(lens), H, cap)).astype(np.float32)
+    wi, wo = c.torch.from_numpy(w_in).to(c.dev), c.torch.full((len(lens), H, cap), -3.0, device=c.dev)
+    got = c.attend(q, rows, name, w_in=wi, w_out=wo)
+    _check_attention(c, kv, q, rows, name, got, D ** -0.5, w=wo.cpu().numpy().astype(np.float64), w_in=w_in)
+    # in place, and from nothing: the same numbers
+    c.attend(q, rows, name, w_in=wi, w_out=wi)
+    for s, n in enumerate(lens):
+        assert c.torch.equal(wi[s, :, :n], wo[s, :, :n])
+    wn = c.torch.full_like(wo, -3.0)
+    again = c.attend(q, rows, name, w_out=wn)
+    assert np.array_equal(again, got)
+    _check_attention(c, kv, q, rows, name, again, D ** -0.5, w=wn.cpu().numpy().astype(np.float64))
+    # unaligned rows with a stride of their own
+    odd = c.attend(q, rows, name, stride=heads * D + 3, shift=1)
+    assert np.array_equal(odd, got)
+
+
+def test_attention_long_with_a_bound_on_the_length():
+    c = Case(2, 128, 128, [9000])
+    kv = c.fill([9000])
+    q = np.random.default_rng(0).standard_normal((3, 4, 128)).astype(np.float32) * 2
+    for max_len in (9000, 12000, 8999, 5000, 128, 1):
+        got = c.attend(q, [3], "f32", max_len=max_len, scale=0.2)
+        _check_attention(c, kv, q, [3], "f32", got, 0.2, max_len=max_len)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.1, 30.0])
+def test_scales(scale):
+    """No temperature, a negative one, one that leaves a single token."""
+    c = Case(2, 64, 16, [200])
+    kv = c.fill([200], scale=0.3)
+    q = np.random.default_rng(0).standard_normal((2, 2, 64)).astype(np.float32)
+    _check_attention(c, kv, q, [2], "f32", c.attend(q, [2], "f32", scale=scale), scale)
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-4, 1e4, 1e25])
+def test_sizes_of_queries_and_values(size):
+    """Queries of any size (the scale takes it back) and values near both ends of the halves."""
+    c = Case(2, 128, 32, [150])
+    vs = 1e-3 if size < 1 else 2000.0
+    kv = c.fill([150], scale=vs)
+    q = (np.random.default_rng(0).standard_normal((2, 4, 128)) * size).astype(np.float32)
+    scale = 0.2 / (size * vs)
+    scale = float(np.float32(scale))
+    _check_attention(c, kv, q, [2], "f32", c.attend(q, [2], "f32", scale=scale), scale)
+
+
+def test_values_of_very_different_sizes_in_one_sequence():
+    """Tokens whose values are a million times those before them, first seen late: what was summed is rescaled."""
+    c = Case(1, 128, 16, [400])
+    rng = np.random.default_rng(2)
+    x = rng.standard_normal((400, 1, 128)).astype(np.float32)
+    v = (x * np.where(np.arange(400) % 97 == 96, 3e3, 1e-3)[:, None, None]).astype(np.float32)
+    c.set_lens([400])
+    c.B.op_kv4_append(c.cache, c.rows(x, "f32"), c.rows(v, "f32"), c.starts([400]))
+    kv = [(O.quantise(x), O.quantise(v))]
+    q = rng.standard_normal((9, 1, 128)).astype(np.float32) * 3
+    _check_attention(c, kv, q, [9], "f32", c.attend(q, [9], "f32"), 128 ** -0.5)
+
+
+def test_rows_without_tokens_and_rows_outside():
+    c = Case(2, 64, 16, [40, 16, 40])
+    kv = c.fill([3, 0, 20])
+    q = np.random.default_rng(0).standard_normal((20, 4, 64)).astype(np.float32)
+    # rows 2..6 for three tokens (the first two see nothing), 7..8 of the empty sequence, 9..14; 0, 1 and 15.. belong to nobody
+    starts = c.torch.tensor([2, 7, 9, 15], dtype=c.torch.int32, device=c.dev)
+    out = c.rows(np.full(q.shape, 777.0, np.float32), "f32")
+    work = c.torch.empty(c.B.op_kv4_work_bytes(c.cache, 20, 4, 40), dtype=c.torch.uint8, device=c.dev)
+    wo = c.torch.full((3, 2, c.cache.capacity), -3.0, device=c.dev)
+    c.B.op_kv4_attention(c.cache, c.rows(q, "f32"), starts, out, 40, work, weights_out=wo)
+    c.torch.cuda.synchronize()
+    got = out.cpu().numpy().astype(np.float64)
+    assert (got[:2] == 777).all() and (got[15:] == 777).all()
+    assert (got[2:4] == 0).all() and (got[7:9] == 0).all()
+    _check_attention(c, kv, q[2:15], [5, 2, 6], "f32", got[2:15], 0.125, w=wo.cpu().numpy().astype(np.float64))
+
+
+def test_no_rows_at_all_carries_the_weights_over():
+    c = Case(2, 64, 16, [40])
+    c.fill([21])
+    wi, wo = c.torch.rand(1, 2, c.cache.capacity, device=c.dev), c.torch.full((1, 2, c.cache.capacity), -3.0, device=c.dev)
+    c.attend(np.zeros((0, 2, 64), np.float32), [0], "f32", w_in=wi, w_out=wo)
+    assert c.torch.equal(wo[..., :21], wi[..., :21]) and (wo[..., 21:] == -3).all()
+
+
+def test_missing_pages_are_seen_by_no_row():
+    c = Case(2, 128, 16, [100, 100])
+    kv = c.fill([100, 90])
+    for bad in ({(0, 0): -1, (0, 3): c.n_pages, (1, 5): 1 << 30}, {(1, i): -1 for i in range(6)}):
+        t = c.table.copy()
+        here = [np.ones(100, bool), np.ones(90, bool)]
+        for (s, i), v in bad.items():
+            t[s, i] = v
+            here[s][16 * i:16 * i + 16] = False
+        c.cache.page_table.copy_(c.torch.from_numpy(t))
+        for rows in ([2, 3], [40, 90]):
+            q = np.random.default_rng(0).standard_normal((sum(rows), 2, 128)).astype(np.float32)
+            wo = c.torch.full((2, 2, c.cache.capacity), -3.0, device=c.dev)
+            got = c.attend(q, rows, "f32", w_out=wo)
+            _check_attention(c, kv, q, rows, "f32", got, 128 ** -0.5, here=here, w=wo.cpu().numpy().astype(np.float64))
+
+
+@pytest.mark.parametrize("rows", [6, 45])
+@pytest.mark.parametrize("kind", ["k", "v"])
+def test_a_token_that_is_not_finite_shows_only_where_it_is_seen(kind, rows):
+    c = Case(2, 128, 16, [60])
+    rng = np.random.default_rng(1)
+    x = [rng.standard_normal((50, 2, 128)).astype(np.float32) for _ in range(2)]
+    bad = 50 - 4
+    x[kind == "v"][bad, 1, 70] = np.inf
+    c.set_lens([50])
+    c.B.op_kv4_append(c.cache, c.rows(x[0], "f32"), c.rows(x[1], "f32"), c.starts([50]))
+    q = rng.standard_normal((rows, 4, 128)).astype(np.float32)
+    got = c.attend(q, [rows], "f32")
+    sees = 50 - rows + np.arange(rows) >= bad
+    assert np.isfinite(got[~sees]).all() and np.isfinite(got[:, :2]).all()
+    part = got[sees][:, 2:]
+    assert np.isnan(part).all() if kind == "k" else (np.isnan(part[..., 64:96]).all() and np.isfinite(part[..., :64]).all() and np.isfinite(part[..., 96:]).all())
+    # every other row has the numbers it has without that token
+    x[kind == "v"][bad, 1, 70] = 0.0
+    kv = [(O.quantise(x[0]), O.quantise(x[1]))]
+    want, tol, _ = O.attention(q.astype(np.float64), kv[0][0], kv[0][1], 50 - rows + np.arange(rows), 128 ** -0.5)
+    assert (np.abs(got - want)[~sees] <= tol[~sees] + np.abs(want[~sees]) * 2.0 ** -24).all()
+
+
+@pytest.mark.parametrize("H,heads,D,n", [(4, 4, 128, 700), (2, 4, 64, 131)])
+def test_a_rows_bits_do_not_depend_on_the_rows_beside_it(H, heads, D, n):
+    """A verification row is the row of one-token decoding, bit for bit (a draft is accepted or not by these numbers)."""
+    c = Case(H, D, 128, [n + 8])
+    c.fill([n + 7])
+    q = np.random.default_rng(0).standard_normal((8, heads, D)).astype(np.float32)
+    c.set_lens([n + 7])
+    many = c.attend(q, [8], "f32", max_len=n + 8)
+    for i in range(8):
+        c.set_lens([n + i])
+        assert np.array_equal(c.attend(q[i:i + 1], [1], "f32", max_len=n + 8)[0], many[i]), i
+
+
+def test_pages_far_apart():
+    """Offsets beyond 32 bits: pages 2.5 GB apart."""
+    import torch
+    from paper_2404_18911_amd import binding as B
+    H, D, T, n = 2, 128, 16, 60
+    c = Case(H, D, T, [n])
+    kv = c.fill([n])
+    stride = (5 << 29) + 4096
+    big = torch.empty(3 * stride + c.block, dtype=torch.uint8, device="cuda:0")
+    order = [2, 0, 3, 1]
+    for i in range(4):
+        big[order[i] * stride:order[i] * stride + c.block] = c.pool[int(c.table[0, i]) * c.stride:int(c.table[0, i]) * c.stride + c.block]
+    c.cache = B.Kv4Cache(big, torch.tensor([order], dtype=torch.int32, device="cuda:0"), c.lens, H, D, T, page_stride=stride)
+    assert c.cache.n_pages == 4
+    q = np.random.default_rng(0).standard_normal((20, 2, D)).astype(np.float32)
+    for rows in (1, 20):
+        wo = torch.full((1, H, c.cache.capacity), -3.0, device="cuda:0")
+        got = c.attend(q[:rows], [rows], "f32", w_out=wo)
+        _check_attention(c, kv, q[:rows], [rows], "f32", got, D ** -0.5, w=wo.cpu().numpy().astype(np.float64))
+    x = np.random.default_rng(3).standard_normal((n, H, D)).astype(np.float32)
+    B.op_kv4_append(c.cache, c.rows(x, "f32"), c.rows(-x, "f32"), c.starts([n]))
+    k, v = c.rows(np.zeros_like(x), "f32"), c.rows(np.zeros_like(x), "f32")
+    B.op_kv4_read(c.cache, c.starts([n]), k, v)
+    assert np.allclose(k.cpu().numpy(), O.values(O.quantise(x)), rtol=2.0 ** -23, atol=0)
+
+
+# ---- eviction -----------------------------------------------------------------------------------
+
+def _tokens(pages, s, H, idx):
+    return [[pages.token(s, h, int(t)) for t in idx[h]] for h in range(H)]
+
+
+@pytest.mark.parametrize("H,D,T,T2,lens,keep,first,recent", [
+    (1, 64, 16, 16, [1], 1, 0, 0), (2, 128, 16, 32, [50, 7, 0], 10, 2, 3), (3, 64, 32, 16, [100], 33, 0, 0), (1, 128, 128, 128, [300], 299, 4, 100),
+    (2, 64, 64, 64, [1100, 40], 40, 40, 0), (1, 64, 16, 16, [70], 21, 0, 21), (2, 128, 16, 16, [3000], 1025, 4, 64)])
+@pytest.mark.parametrize("kind", ["random", "ties", "zeros", "odd"])
+def test_evict(H, D, T, T2, lens, keep, first, recent, kind):
+    c = Case(H, D, T, [n + 5 for n in lens], seed=1)
+    d = Case(H, D, T2, [keep + 3] * len(lens), seed=2)
+    c.fill(lens)
+    rng = np.random.default_rng(4)
+    w = np.exp(rng.standard_normal((len(lens), H, c.cache.capacity)) * 2).astype(np.float32)
+    if kind == "ties":
+        w = rng.integers(0, 4, w.shape).astype(np.float32)
+    elif kind == "zeros":
+        w[:] = 0
+    elif kind == "odd":
+        w = rng.standard_normal(w.shape).astype(np.float32)
+        w[rng.random(w.shape) < 0.2] = -0.0
+        w[rng.random(w.shape) < 0.2] = 0.0
+        for v in (np.nan, np.inf, -np.inf, 1e-42):
+            w[rng.random(w.shape) < 0.05] = v
+        w.view(np.uint32)[np.isnan(w) & (rng.random(w.shape) < 0.5)] = 0xFFC00001      # a negative NaN
+    wi = c.torch.from_numpy(w).to(c.dev)
+    wo = c.torch.full((len(lens), H, d.cache.capacity), -3.0, device=c.dev)
+    kept = c.torch.full((len(lens), H, keep), 99, dtype=c.torch.int32, device=c.dev)
+    src_before, dst_before = c.pool.clone(), d.pool.cpu().numpy().copy()
+    c.B.op_kv4_evict(c.cache, d.cache, keep, first, recent, wi, wo, kept)
+    c.torch.cuda.synchronize()
+    assert c.torch.equal(c.pool, src_before)
+    kept, wo = kept.cpu().numpy(), wo.cpu().numpy()
+    a, b = c.host(), d.host()
+    touched = np.zeros(len(dst_before), bool)
+    for s, n in enumerate(lens):
+        m = min(n, keep)
+        for h in range(H):
+            want = O.evict(w[s, h].astype(np.float64), n, keep, first, recent)
+            assert np.array_equal(kept[s, h, :m], want), (s, h)
+            assert (kept[s, h, m:] == -1).all()
+            assert np.array_equal(wo[s, h, :m].view(np.uint32), w[s, h, want].view(np.uint32)) and (wo[s, h, m:] == 0).all()
+            for i in range(0, m, 1 if m < 200 else 37):
+                for x, y in zip(a.token(s, h, int(want[i])), b.token(s, h, i)):
+                    assert all(np.array_equal(p, q, equal_nan=True) for p, q in zip(x, y)), (s, h, i)
+            for i in range(m):
+                touched[[int(d.table[s, i // T2]) * d.stride + o for o in O.token_offsets(H, D, T2, h, i % T2)]] = True
+    assert (b.pool[~touched] == dst_before[~touched]).all()
+
+
+def test_evict_within_one_pool_and_missing_pages():
+    """dst pages in the pool that src is in; a token whose page is missing is kept as zeros, a missing dst page is skipped."""
+    import torch
+    from paper_2404_18911_amd import binding as B
+    c = Case(2, 64, 16, [64], spare=6)
+    c.fill([64])
+    free = sorted(set(range(c.n_pages)) - set(int(p) for p in c.table[0, :4]))
+    dst = B.Kv4Cache(c.pool, torch.tensor([[free[3], -1, free[1]]], dtype=torch.int32, device=c.dev), torch.zeros(1, dtype=torch.int32, device=c.dev), 2, 64, 16)
+    t = c.table.copy()
+    t[0, 1] = -1
+    c.cache.page_table.copy_(torch.from_numpy(t))
+    before = c.host()
+    w = torch.rand(1, 2, c.cache.capacity, device=c.dev)
+    kept = torch.zeros(1, 2, 40, dtype=torch.int32, device=c.dev)
+    B.op_kv4_evict(c.cache, dst, 40, 18, 2, w, torch.empty(1, 2, 48, device=c.dev), kept)
+    torch.cuda.synchronize()
+    kept, after = kept.cpu().numpy(), c.host()
+    after.table = np.array([[free[3], -1, free[1]]])
+    for h in range(2):
+        assert np.array_equal(kept[0, h], O.evict(w[0, h].cpu().numpy().astype(np.float64), 64, 40, 18, 2))
+        for i in list(range(16)) + list(range(32, 40)):
+            f = int(kept[0, h, i])
+            got = after.token(0, h, i)
+            if 16 <= f < 32:
+                assert all((p == 0).all() for x in got for p in x)
+            else:
+                before.table = c.table
+                assert all(np.array_equal(p, q) for x, y in zip(got, before.token(0, h, f)) for p, q in zip(x, y))
+
+
+# ---- together -----------------------------------------------------------------------------------
+
+def _model_step(st, x_k, x_v):
+    return [tuple(np.concatenate([a, b]) for a, b in zip(st[i], O.quantise((x_k, x_v)[i]))) for i in range(2)]
+
+
+STEPS = [40, 1, 3, 1, 1, 7, 1, 20, 1, 5, 8, 1, 1]                 # 72 tokens at the eighth, then 48 .. 64
+
+
+@pytest.mark.parametrize("steps,n_evictions", [(STEPS, 1), (STEPS + [2, 1, 7], 2)])
+@pytest.mark.parametrize("name,H,heads,D,T", [("f32", 2, 2, 128, 16), ("bf16", 2, 8, 64, 32)])
+def test_a_request_with_a_bounded_cache(name, H, heads, D, T, steps, n_evictions):
+    """A prompt, decode and verification steps of several rows with rollback, evictions, and on: every output against the
+    definition followed on the CPU, the kept tokens as the device's own weights say."""
+    import torch
+    from paper_2404_18911_amd import binding as B
+    rng = np.random.default_rng(11)
+    budget, cap = 48, 96
+    cur, other = Case(H, D, T, [cap], seed=1), Case(H, D, T, [cap], seed=2)
+    state = [(np.zeros((0, H, D // 32, 32)), np.zeros((0, H, D // 32)), np.zeros((0, H, D // 32))) for _ in range(2)]
+    w = torch.zeros(1, H, cur.cache.capacity, device=cur.dev)
+    n = 0
+    evictions = 0
+    for step, r in enumerate(steps):
+        xk, xv = (O.ROUND[name](rng.standard_normal((r, H, D)).astype(np.float32)) for _ in range(2))
+        q = O.ROUND[name](rng.standard_normal((r, heads, D)).astype(np.float32) * 2)
+        n += r
+        cur.set_lens([n])
+        B.op_kv4_append(cur.cache, cur.rows(xk, name), cur.rows(xv, name), cur.starts([r]))
+        w_before = w.cpu().numpy().copy()
+        got = cur.attend(q, [r], name, max_len=cap, w_in=w, w_out=w)
+        state = _model_step(state, xk, xv)
+        wn = w.cpu().numpy().astype(np.float64)
+        want, tol, prob = O.attention(q.astype(np.float64), state[0], state[1], n - r + np.arange(r), D ** -0.5)
+        assert (np.abs(got - want) <= tol + O.HALF_STEP[name] * np.abs(want)).all(), step
+        add = prob.reshape(r, H, heads // H, n).sum((0, 2))
+        assert np.allclose(wn[0, :, :n], w_before[0, :, :n] + add, rtol=1e-4, atol=1e-6)
+        if r == 3:                                            # a draft was rejected: two tokens fewer, nothing else to do
+            n -= 2
+            state = [tuple(a[:n] for a in t) for t in state]
+            w[0, :, n:] = 0
+        if n > 64:
+            kept = torch.empty(1, H, budget, dtype=torch.int32, device=cur.dev)
+            w2 = torch.empty(1, H, other.cache.capacity, device=cur.dev)
+            B.op_kv4_evict(cur.cache, other.cache, budget, 4, 8, w, w2, kept)
+            idx = kept.cpu().numpy()[0]
+            for h in range(H):
+                assert np.array_equal(idx[h], O.evict(w[0, h].cpu().numpy().astype(np.float64), n, budget, 4, 8))
+            state = [tuple(np.stack([a[idx[h], h] for h in range(H)], 1) for a in t) for t in state]
+            cur, other, w, n = other, cur, w2, budget
+            evictions += 1
+    assert evictions == n_evictions
+
+
+@pytest.mark.parametrize("grow", [1, 9])
+def test_a_captured_step_follows_lengths_and_pages_that_change(grow):
+    """append, attention and eviction in one graph, replayed while the lengths in device memory grow; eager work between.  (A length that
+    grows by more than the rows appended takes in tokens that nobody wrote: NaN, compared as bits like everything else.)"""
+    import torch
+    from paper_2404_18911_amd import binding as B
+    H, D, T, cap = 2, 128, 16, 128
+    c, d, ref = Case(H, D, T, [cap, cap], seed=1), Case(H, D, T, [32, 32], seed=2), Case(H, D, T, [cap, cap], seed=1)
+    dref = Case(H, D, T, [32, 32], seed=2)
+    lens = [30, 1]
+    c.fill(lens)
+    ref.fill(lens)
+    xk, xv, q = (torch.zeros(3, H, D, device=c.dev) for _ in range(3))
+    out = torch.zeros(3, H, D, device=c.dev)
+    starts = c.starts([2, 1])
+    w, w2 = torch.zeros(2, H, cap, device=c.dev), torch.zeros(2, H, 32, device=c.dev)
+    kept = torch.zeros(2, H, 20, dtype=torch.int32, device=c.dev)
+    work = torch.empty(B.op_kv4_work_bytes(c.cache, 3, H, cap), dtype=torch.uint8, device=c.dev)
+
+    def step(x, y, out, w, w2, kept, work):
+        B.op_kv4_append(x.cache, xk, xv, starts)
+        B.op_kv4_attention(x.cache, q, starts, out, cap, work, weights_in=w, weights_out=w)
+        B.op_kv4_evict(x.cache, y.cache, 20, 2, 5, w, w2, kept)
+    side = torch.cuda.Stream()
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=side):
+        step(c, d, out, w, w2, kept, work)
+    e_out, e_w, e_w2, e_kept, e_work = torch.zeros_like(out), torch.zeros_like(w), torch.zeros_like(w2), torch.zeros_like(kept), torch.empty_like(work)
+    rng = np.random.default_rng(0)
+    for i in range(5):
+        lens = [lens[0] + 2, lens[1] + grow]
+        for x in (c, ref):
+            x.set_lens(lens)
+        for t in (xk, xv, q):
+            t.copy_(torch.from_numpy(rng.standard_normal((3, H, D)).astype(np.float32)))
+        if i == 3:                                            # another page order from here on
+            for x in (c, ref):
+                x.table[:, [0, 2]] = x.table[:, [2, 0]]
+                x.cache.page_table.copy_(torch.from_numpy(x.table))
+        step(ref, dref, e_out, e_w, e_w2, e_kept, e_work)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for got, want in ((out, e_out), (kept, e_kept), (w, e_w), (w2, e_w2)):
+            assert torch.equal(got.view(torch.int32), want.view(torch.int32)), i
+        assert grow > 1 or i >= 3 or out.isfinite().all()       # (the other order brings pages forward that nobody wrote yet)
+        assert torch.equal(c.pool, ref.pool)
+        work.random_(0, 256)                                  # nothing in the workspace is kept between calls
+
+
+def test_calls_go_to_the_current_stream():
+    import torch
+    c = Case(2, 64, 16, [64])
+    kv = c.fill([64])
+    q = np.random.default_rng(0).standard_normal((1, 2, 64)).astype(np.float32)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(10_000_000)
+        c.pool.zero_()                                        # ordered in front of the call on this stream only
+        got = c.attend(q, [1], "f32")
+    assert (got == 0).all()
+    assert kv
+
+
+def test_binding_refusals_on_the_gpu():
+    import torch
+    c = Case(2, 64, 16, [64])
+    B, z = c.B, torch.zeros
+    k = z(1, 2, 64, device=c.dev)
+    st = c.starts([1])
+    work = z(1 << 20, dtype=torch.uint8, device=c.dev)
+    for bad in (z(1, 3, 64, device=c.dev), z(1, 2, 32, device=c.dev), z(2, 2, 64, device=c.dev), z(1, 2, 64), z(1, 2, 64, device=c.dev, dtype=torch.float64),
+                z(1, 2, 64, device=c.dev, dtype=torch.float16), z(1, 2, 128, device=c.dev)[..., ::2]):
+        with pytest.raises(ValueError):
+            B.op_kv4_append(c.cache, k, bad, st)
+        with pytest.raises(ValueError):
+            B.op_kv4_read(c.cache, st, k, bad)
+        with pytest.raises(ValueError):
+            B.op_kv4_attention(c.cache, k, st, bad, 64, work)
+    for bad in (st.long(), st[:1], st.cpu()):
+        with pytest.raises(ValueError):
+            B.op_kv4_append(c.cache, k, k.clone(), bad)
+    for bad in (z(1, 2, 63, device=c.dev), z(1, 2, 64, device=c.dev, dtype=torch.float16), z(1, 2, 64)):
+        with pytest.raises(ValueError):
+            B.op_kv4_attention(c.cache, k, st, k.clone(), 64, work, weights_out=bad)
+    with pytest.raises(B.KangarooError):
+        B.op_kv4_attention(c.cache, k, st, k, 64, work)                          # in place
+    with pytest.raises(B.KangarooError) as e:
+        B.op_kv4_attention(c.cache, k, st, k.clone(), 64, work[:16])
+    assert e.value.code == B.KG_ENOSPC
+    with pytest.raises(ValueError):
+        B.op_kv4_evict(c.cache, c.cache, 4, 0, 0, z(1, 2, 64, device=c.dev), z(1, 2, 64, device=c.dev), z(1, 2, 5, device=c.dev, dtype=torch.int32))
