@@ -2594,16 +2594,43 @@ int kg_op_kv4_read(const kg_kv4_cache *c, int dtype, void *k, long k_stride, voi
     return hipGetLastError() == hipSuccess ? KG_OK : KG_EHIP;
 }
 
+constexpr int KV4_MANY_TILES = 2, KV4_MANY_COLUMNS = 64 * KV4_MANY_TILES;
+
 static bool kv4_attn_shape_ok(const kg_kv4_cache *c, int n_rows, int n_heads, int max_len)
 {
     return kv4_cache_ok(c) && n_rows >= 0 && n_heads >= 1 && n_heads <= KG_KV4_MAX_HEADS && n_heads % c->n_kv_heads == 0 && max_len >= 1 &&
-           max_len <= (1 << 30);
+           max_len <= (1 << 30) && (size_t)n_rows * n_heads < (size_t)1 << 31;
+}
+
+// How the attention is cut.  Few columns (at most 16 a sequence on average): one workgroup of four waves per cache head, 16 columns and chunk
+// of the tokens.  The chunks follow from the arguments that do not change with the rows, so that a row's sums are cut alike whatever
+// stands beside it.
+struct Kv4Plan { bool few; int blocks, chunk, n_chunks; };
+static Kv4Plan kv4_plan(const kg_kv4_cache *c, int n_rows, int n_heads, int max_len)
+{
+    Kv4Plan p;
+    const int group = n_heads / c->n_kv_heads;
+    const long cols = (long)n_rows * group;
+    const int len = (int)std::min<long>(max_len, (long)c->max_pages * c->page_tokens);
+    p.few = cols <= 16L * c->n_seqs;
+    const int cb = p.few ? 16 : KV4_MANY_COLUMNS;
+    // every sequence may end in a block that is not full
+    p.blocks = (int)std::min<long>(cols, (cols + cb - 1) / cb + std::min(c->n_seqs - 1, n_rows - 1));
+    const int unit = 128, units = (len + unit - 1) / unit;
+    const long per_chunk = (long)c->n_kv_heads * (p.few ? c->n_seqs : p.blocks), want = p.few ? 1024 : 512;
+    const long n = std::min<long>(units, std::max<long>(1, want / per_chunk));
+    p.chunk = (int)((units + n - 1) / n) * unit;
+    p.n_chunks = (len + p.chunk - 1) / p.chunk;
+    return p;
 }
 
 size_t kg_op_kv4_work_bytes(const kg_kv4_cache *c, int n_rows, int n_heads, int max_len)
 {
     if (!kv4_attn_shape_ok(c, n_rows, n_heads, max_len)) return 0;
-    return up((size_t)n_rows * n_heads * 4) + ALIGN;
+    if (n_rows == 0) return ALIGN;
+    const Kv4Plan p = kv4_plan(c, n_rows, n_heads, max_len);
+    const size_t lanes = (size_t)n_rows * n_heads;
+    return up(lanes * 4) + up(p.n_chunks > 1 ? lanes * p.n_chunks * (c->head_dim + 2) * 4 : 0);
 }
 
 int kg_op_kv4_attention(const kg_kv4_cache *c, int dtype, const void *q, long q_stride, int n_heads, const int32_t *row_start, int n_rows,
@@ -2624,17 +2651,27 @@ int kg_op_kv4_attention(const kg_kv4_cache *c, int dtype, const void *q, long q_
     if (n_rows == 0 && !weights_out) return KG_OK;
     Kv4Attn a;
     a.c = kv4_view(c); a.q = q; a.out = out; a.q_stride = q_stride; a.out_stride = out_stride; a.row_start = row_start; a.n_rows = n_rows;
-    a.heads = n_heads; a.max_len = (int)std::min<size_t>(max_len, cap); a.scale = scale; a.w_in = weights_in; a.w_out = weights_out; a.lse = (float *)work;
+    a.heads = n_heads; a.group = n_heads / c->n_kv_heads; a.max_len = (int)std::min<size_t>(max_len, cap); a.scale = scale;
+    a.w_in = weights_in; a.w_out = weights_out; a.lse = (float *)work;
+    a.part = (float *)((char *)work + up((size_t)n_rows * n_heads * 4));
     hipStream_t s = (hipStream_t)hip_stream;
     if (n_rows > 0) {
-        const dim3 grid(n_rows, n_heads);
-#define KV4_LAUNCH(T, D) hipLaunchKernelGGL((kv4_attend_kernel<T, D>), grid, dim3(128), 0, s, a)
-        KV4_BY_TYPE_AND_DIM(KV4_LAUNCH, c->head_dim);
-#undef KV4_LAUNCH
+        const Kv4Plan p = kv4_plan(c, n_rows, n_heads, max_len);
+        a.chunk = p.chunk; a.n_chunks = p.n_chunks;
+        const dim3 grid(p.blocks, c->n_kv_heads, p.n_chunks);
+#define KV4_FEW(T, D) hipLaunchKernelGGL((kv4_attend_few_kernel<T, D>), grid, dim3(256), 0, s, a)
+#define KV4_MANY(T, D) hipLaunchKernelGGL((kv4_attend_many_kernel<T, D, KV4_MANY_TILES>), grid, dim3(256), 0, s, a)
+#define KV4_JOIN(T, D) hipLaunchKernelGGL((kv4_join_kernel<T, D>), dim3((unsigned)(((size_t)n_rows * n_heads + 3) / 4)), dim3(256), 0, s, a)
+        if (p.few) KV4_BY_TYPE_AND_DIM(KV4_FEW, c->head_dim);
+        else KV4_BY_TYPE_AND_DIM(KV4_MANY, c->head_dim);
+        if (p.n_chunks > 1) KV4_BY_TYPE_AND_DIM(KV4_JOIN, c->head_dim);
+#undef KV4_FEW
+#undef KV4_MANY
+#undef KV4_JOIN
     }
     if (weights_out) {
-        const dim3 grid((a.max_len + 127) / 128, c->n_kv_heads, c->n_seqs);
-#define KV4_LAUNCH(T, D) hipLaunchKernelGGL((kv4_weights_kernel<T, D>), grid, dim3(128), 0, s, a)
+        const dim3 wgrid((a.max_len + 127) / 128, c->n_kv_heads, c->n_seqs);
+#define KV4_LAUNCH(T, D) hipLaunchKernelGGL((kv4_weights_kernel<T, D>), wgrid, dim3(256), 0, s, a)
         KV4_BY_TYPE_AND_DIM(KV4_LAUNCH, c->head_dim);
 #undef KV4_LAUNCH
     }

@@ -192,99 +192,604 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(const Kv4View c, T *k, lo
     }
 }
 
+// ---- attention ----------------------------------------------------------------------------------
+//
+// A wave takes 16 NC columns, a column being one row and query head of a sequence and cache head, over steps of 32 tokens (two tiles of 16).
+//   scores   z[t][c] = f_c (sum_g s_tg (n_t . q_c)_g + m_tg . (sum of q_c)_g): the levels n are exact in fp16, so a group's 32 products are one
+//            matrix instruction for each of two fp16 parts of the query (scaled by a power of two to below 2^10: the parts hold 22
+//            bits), its scale a multiplication in fp32; the minima are one more instruction over the groups, whose result the others add to.
+//   softmax  over steps with a running reference M_c, the largest z_t + e_t seen, e_t the exponent of the token's largest value scale:
+//            2^(z - M + 14) s is then below 2^14 whatever the sizes of values and scales, and as two fp16 parts is held to 22 bits
+//            and 2^-39 of the largest.
+//   values   o[d][c] = sum_t n_td (p_t s_tg)_c as matrix instructions, the levels again exact; sum_t p_t m_tg in fp32.
+// The scores of a lane (column lane % 16, tokens 4 (lane / 16) + 0..3 of both tiles) are the products' side of the second matrix
+// instruction, so probabilities never leave the lane.
 struct Kv4Attn {
     Kv4View c;
     const void *q;
     void *out;
     long q_stride, out_stride;
     const int *row_start;
-    int n_rows, heads, max_len;
+    int n_rows, heads, group, max_len;      // group: query heads of a cache head
+    int chunk, n_chunks;                    // tokens of a workgroup; of the few-columns kernel a multiple of 128
     float scale;
     const float *w_in;
-    float *w_out, *lse;          // lse [row][head], base 2
+    float *w_out, *lse;                     // lse [row][head], base 2
+    float *part;                            // [n_chunks][row][head][D + 2]: sums, reference, sum of the probabilities
 };
 
-// One row and head per workgroup, a token per thread.
-template <typename T, int D>
-__global__ __launch_bounds__(128) void kv4_attend_kernel(const Kv4Attn a)
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+union Kv4Op { uint32_t w[4]; f16x8_t v; };
+
+// across the four lanes of a column
+__device__ __forceinline__ float quads_max(float v)
 {
-    typedef Kv4<D> L;
-    __shared__ float qs[D], ps[128], red[2];
-    const int r = blockIdx.x, hq = blockIdx.y, h = hq / (a.heads / a.c.H), P = 1 << a.c.logT, tid = threadIdx.x;
-    const Kv4Row row = kv4_row(a.c, a.row_start, r);
-    if (row.s < 0) return;
-    for (int d = tid; d < D; d += 128) qs[d] = row_ld((const T *)a.q + (size_t)r * a.q_stride + (size_t)hq * D + d) * (a.scale * 1.44269504f);
-    __syncthreads();
-    const int n = min(row.pos + 1, a.max_len);
-    float mx = -INFINITY, l = 0.f, o = 0.f;
-    for (int t0 = 0; t0 < n; t0 += 128) {
-        const int t = t0 + tid;
-        float sc = -INFINITY;
-        const char *blk = t < n ? kv4_block<D>(a.c, row.s, h, t) : nullptr;
-        if (blk) {
-            const int tp = t & (P - 1);
-            sc = 0.f;
-            for (int d = 0; d < D; d++) {
-                const int g = d >> 5;
-                const uint32_t kw = *(const uint32_t *)(blk + L::k_word(P, tp, (d & 31) >> 3, g)) >> (4 * (d & 7)) & 15;
-                sc = fmaf(qs[d], fmaf((float)*(const _Float16 *)(blk + L::ks(P, tp, g)), (float)kw, (float)*(const _Float16 *)(blk + L::km(P, tp, g))), sc);
-            }
-        }
-        float m = sc;
-        for (int i = 1; i < 64; i <<= 1) m = fmaxf(m, __shfl_xor(m, i));
-        if ((tid & 63) == 0) red[tid >> 6] = m;
-        __syncthreads();
-        m = fmaxf(mx, fmaxf(red[0], red[1]));
-        const float p = blk ? exp2f(sc - m) : 0.f;
-        ps[tid] = p;
-        __syncthreads();
-        const float alpha = mx == -INFINITY ? 0.f : exp2f(mx - m);
-        mx = m;
-        o *= alpha; l *= alpha;
-        for (int i = 0; i < 128 && t0 + i < n; i++) {
-            l += ps[i];
-            const char *b = kv4_block<D>(a.c, row.s, h, t0 + i);
-            if (!b || tid >= D) continue;
-            const int j = tid >> 4, tp = (t0 + i) & (P - 1);
-            const uint32_t vw = *(const uint16_t *)(b + L::v_half(P, tp, tid & 15, j >> 2)) >> (4 * (j & 3)) & 15;
-            o = fmaf(ps[i], fmaf((float)*(const _Float16 *)(b + L::vs(P, tp, tid >> 5)), (float)vw, (float)*(const _Float16 *)(b + L::vm(P, tp, tid >> 5))), o);
-        }
-        __syncthreads();
-    }
-    if (tid < D) ((T *)a.out)[(size_t)r * a.out_stride + (size_t)hq * D + tid] = (T)(l == 0.f ? 0.f : o / l);
-    if (tid == 0) a.lse[(size_t)r * a.heads + hq] = l == 0.f ? -INFINITY : mx + log2f(l);
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return pair_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float quads_sum(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+// levels i and i + 4 of a word as halves, i = 0..3
+__device__ __forceinline__ void kv4_widen(uint32_t w, uint32_t (&o)[4])
+{
+    const f16x2_t one = {(_Float16)1024, (_Float16)1024}, sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f}, sixty_four = {(_Float16)64, (_Float16)64};
+    const uint32_t hi = w >> 8;
+    // 1024 + n, or 1024 + 16 n of the nibble above
+    const f16x2_t a = __builtin_bit_cast(f16x2_t, (w & 0x000f000fu) | 0x64006400u), b = __builtin_bit_cast(f16x2_t, (w & 0x00f000f0u) | 0x64006400u);
+    const f16x2_t c = __builtin_bit_cast(f16x2_t, (hi & 0x000f000fu) | 0x64006400u), d = __builtin_bit_cast(f16x2_t, (hi & 0x00f000f0u) | 0x64006400u);
+    o[0] = __builtin_bit_cast(uint32_t, a - one);
+    o[1] = __builtin_bit_cast(uint32_t, b * sixteenth - sixty_four);
+    o[2] = __builtin_bit_cast(uint32_t, c - one);
+    o[3] = __builtin_bit_cast(uint32_t, d * sixteenth - sixty_four);
+}
+__device__ __forceinline__ float half_of(uint32_t w, int i) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(i ? w >> 16 : w)); }
+
+// two fp16 parts of a pair of numbers, rounded towards zero (the second takes what the first leaves)
+__device__ __forceinline__ void kv4_split(float x, float y, uint32_t &hi, uint32_t &lo)
+{
+#pragma clang fp contract(off)
+    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, y));
+    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x - half_of(hi, 0), y - half_of(hi, 1)));
 }
 
-// w_out[s][h][t] = w_in + the probabilities of token t, summed over the rows and the query heads of head h.  A thread per token.
-template <typename T, int D>
-__global__ __launch_bounds__(128) void kv4_weights_kernel(const Kv4Attn a)
+// The columns of a block: sequence, first column, how many of the sequence's there are.
+struct Kv4Cols { int s, c0, n, r0, end; };
+template <int CB> __device__ __forceinline__ Kv4Cols kv4_columns(const Kv4Attn &a, int block)
 {
-    typedef Kv4<D> L;
-    __shared__ float qs[D];
-    const int s = blockIdx.z, h = blockIdx.y, t = blockIdx.x * 128 + threadIdx.x, P = 1 << a.c.logT, g = a.heads / a.c.H;
-    const int len = kv4_len(a.c, s), n = min(len, a.max_len);
-    if ((int)blockIdx.x * 128 >= n) return;
-    const char *blk = t < n ? kv4_block<D>(a.c, s, h, t) : nullptr;
-    const size_t at = ((size_t)s * a.c.H + h) * ((size_t)a.c.max_pages << a.c.logT) + t;
-    float sum = 0.f;
-    const int r0 = max(a.row_start[s], 0), r1 = min(a.row_start[s + 1], a.n_rows);
-    for (int r = r0; r < r1; r++) {
-        for (int hq = h * g; hq < h * g + g; hq++) {
-            __syncthreads();
-            for (int d = threadIdx.x; d < D; d += 128) qs[d] = row_ld((const T *)a.q + (size_t)r * a.q_stride + (size_t)hq * D + d) * (a.scale * 1.44269504f);
-            __syncthreads();
-            if (!blk || t > len - a.row_start[s + 1] + r) continue;
-            float sc = 0.f;
-            const int tp = t & (P - 1);
-            for (int d = 0; d < D; d++) {
-                const int gr = d >> 5;
-                const uint32_t kw = *(const uint32_t *)(blk + L::k_word(P, tp, (d & 31) >> 3, gr)) >> (4 * (d & 7)) & 15;
-                sc = fmaf(qs[d], fmaf((float)*(const _Float16 *)(blk + L::ks(P, tp, gr)), (float)kw, (float)*(const _Float16 *)(blk + L::km(P, tp, gr))), sc);
-            }
-            sum += exp2f(sc - a.lse[(size_t)r * a.heads + hq]);
+    const int lane = threadIdx.x & 63;
+    int done = 0;
+    for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) {
+        const int s = s0 + lane;
+        int r0 = 0, end = 0, rows = 0;
+        if (s < a.c.n_seqs) {
+            r0 = a.row_start[s]; end = a.row_start[s + 1];
+            const int lo = min(max(r0, 0), a.n_rows);
+            rows = min(max(end, lo), a.n_rows) - lo;
+            r0 = lo;
+        }
+        const int nb = (rows * a.group + CB - 1) / CB;
+        int sum = nb;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int u = __shfl_up(sum, o);
+            if (lane >= o) sum += u;
+        }
+        const unsigned long long hit = __ballot(done + sum > block);
+        if (hit) {
+            const int l = __builtin_ctzll(hit);
+            Kv4Cols k;
+            k.s = s0 + l;
+            k.c0 = (block - done - __builtin_amdgcn_readlane(sum - nb, l)) * CB;
+            k.n = __builtin_amdgcn_readlane(rows, l) * a.group;
+            k.r0 = __builtin_amdgcn_readlane(r0, l);
+            k.end = __builtin_amdgcn_readlane(end, l);
+            return k;
+        }
+        done += __builtin_amdgcn_readlane(sum, 63);
+    }
+    return {-1, 0, 0, 0, 0};
+}
+
+// eight elements of a row
+template <typename T> __device__ __forceinline__ void kv4_load8(const T *p, bool aligned, float (&x)[8])
+{
+    if (aligned) {
+        typedef T vec_t __attribute__((ext_vector_type(8)));
+        const vec_t v = *(const vec_t *)p;
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[e] = (float)v[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[e] = (float)p[e];
+    }
+}
+
+// One column tile's queries: the products' side of the score instructions.
+template <int D> struct Kv4Query {
+    Kv4Op hi[D / 32], lo[D / 32], sum;      // slot 2 i, 2 i + 1 of lane group q: components 8 q + i, 8 q + i + 4 of the group
+    float f;                                // what a sum of products is worth as a base-2 exponent
+
+    template <typename T> __device__ __forceinline__ void load(const T *row, bool live, bool aligned, float scale, int q)
+    {
+        constexpr int G = D / 32;
+        float x[G][8], mx = 0.f;
+#pragma unroll
+        for (int g = 0; g < G; g++) {
+#pragma unroll
+            for (int e = 0; e < 8; e++) x[g][e] = 0.f;
+            if (live) kv4_load8(row + 32 * g + 8 * q, aligned, x[g]);
+#pragma unroll
+            for (int e = 0; e < 8; e++) mx = fmaxf(mx, fabsf(x[g][e]));
+        }
+        mx = quads_max(mx);
+        const int ex = mx > 0.f && mx <= 3.402823466e38f ? __builtin_amdgcn_frexp_expf(mx) : 10;
+        f = __builtin_amdgcn_ldexpf(scale * 1.44269504088896341f, ex - 10);
+        uint32_t sh[2] = {0, 0}, sl[2] = {0, 0};
+        float total[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int g = 0; g < G; g++) {
+            float t = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; e++) { x[g][e] = __builtin_amdgcn_ldexpf(x[g][e], 10 - ex); t += x[g][e]; }
+#pragma unroll
+            for (int i = 0; i < 4; i++) kv4_split(x[g][i], x[g][i + 4], hi[g].w[i], lo[g].w[i]);
+            total[g] = quads_sum(t);
+        }
+        kv4_split(total[0], total[1], sh[0], sl[0]);
+        kv4_split(total[2], total[3], sh[1], sl[1]);
+        sum.w[0] = q == 0 ? sh[0] : 0; sum.w[1] = q == 0 ? sh[1] : 0;       // groups 0..3 against the minima's slots 0..3 and 4..7
+        sum.w[2] = q == 0 ? sl[0] : 0; sum.w[3] = q == 0 ? sl[1] : 0;
+    }
+};
+
+// The numbers of one tile of 16 tokens as they lie in the page.
+template <int D> struct Kv4Keys {
+    static constexpr int G = D / 32;
+    uint32_t w[G], s[2 * G], m[G / 2];      // lane's token: words; tokens 4 q + 0..3: scales; lane's token: minima
+
+    __device__ __forceinline__ void load(const char *blk, int P, int t, int lane)
+    {
+        const int q = lane >> 4, tok = t + (lane & 15);
+        __builtin_memcpy(w, __builtin_assume_aligned(blk + Kv4<D>::k_word(P, tok, q, 0), 4 * G), 4 * G);
+        __builtin_memcpy(s, __builtin_assume_aligned(blk + Kv4<D>::ks(P, t + 4 * q, 0), 16), 8 * G);
+        __builtin_memcpy(m, __builtin_assume_aligned(blk + Kv4<D>::km(P, tok, 0), 2 * G), 2 * G);
+    }
+    // the levels as the other side of the score instructions
+    __device__ __forceinline__ void widen(f16x8_t (&k)[G]) const
+    {
+#pragma unroll
+        for (int g = 0; g < G; g++) {
+            Kv4Op o;
+            kv4_widen(w[g], o.w);
+            k[g] = o.v;
         }
     }
-    if (t < n) a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + sum;
+    // scores of tokens 4 q + 0..3 in the units of Kv4Query::f
+    __device__ __forceinline__ f32x4_t scores(const f16x8_t (&k)[G], const Kv4Query<D> &x) const
+    {
+        Kv4Op mm;
+        mm.w[0] = mm.w[2] = m[0];
+        mm.w[1] = mm.w[3] = G == 4 ? m[G / 2 - 1] : 0;
+        const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+        f32x4_t z = __builtin_amdgcn_mfma_f32_16x16x32_f16(mm.v, x.sum.v, zero, 0, 0, 0);
+#pragma unroll
+        for (int g = 0; g < G; g++) {
+            f32x4_t d = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[g], x.hi[g].v, zero, 0, 0, 0);
+            d = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[g], x.lo[g].v, d, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; i++) z[i] = fmaf(half_of(s[2 * g + (i >> 1)], i & 1), d[i], z[i]);
+        }
+        return z;
+    }
+};
+template <int D> struct Kv4Values {
+    static constexpr int G = D / 32, VH = D / 64;
+    uint32_t w[2 * VH], s[2 * G], m[2 * G]; // tokens 4 q + 0..3: words of lane % 16, scales, minima
+
+    __device__ __forceinline__ void load(const char *blk, int P, int t, int lane)
+    {
+        const int q = lane >> 4;
+        __builtin_memcpy(w, __builtin_assume_aligned(blk + Kv4<D>::v_half(P, t + 4 * q, lane & 15, 0), 8 * VH), 8 * VH);
+        __builtin_memcpy(s, __builtin_assume_aligned(blk + Kv4<D>::vs(P, t + 4 * q, 0), 16), 8 * G);
+        __builtin_memcpy(m, __builtin_assume_aligned(blk + Kv4<D>::vm(P, t + 4 * q, 0), 16), 8 * G);
+    }
+    // exponents of the tokens' largest scales (of garbage: some finite number)
+    __device__ __forceinline__ void exponents(float (&e)[4]) const
+    {
+#pragma unroll
+        for (int a = 0; a < 2; a++) {
+            f16x2_t mx = __builtin_bit_cast(f16x2_t, s[a]);
+#pragma unroll
+            for (int g = 1; g < G; g++) mx = __builtin_elementwise_max(mx, __builtin_bit_cast(f16x2_t, s[2 * g + a]));
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const int ex = (int)(__builtin_bit_cast(uint32_t, mx) >> (16 * i + 10) & 31);      // s < 2^(ex - 14)
+                e[2 * a + i] = (float)(ex - 14);
+            }
+        }
+    }
+};
+
+// The step's two tiles: where they lie (null: no page, none of its tokens is seen).
+struct Kv4Step { const char *blk[2]; int t[2]; bool here[2]; };
+template <int D> __device__ __forceinline__ Kv4Step kv4_step(const Kv4View &c, int s, int h, int t0, int limit)
+{
+    Kv4Step st;
+    const int P = 1 << c.logT;
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        const int t = t0 + 16 * i;
+        int page = -1;
+        if (t < limit) page = c.table[(size_t)s * c.max_pages + (t >> c.logT)];
+        page = __builtin_amdgcn_readfirstlane(page);
+        st.here[i] = page >= 0 && page < c.n_pages;
+        st.t[i] = st.here[i] ? t & (P - 1) : 0;                 // (a tile that is not there is read as page 0 and masked)
+        st.blk[i] = c.pool + (size_t)(st.here[i] ? page : 0) * c.page_stride + (size_t)h * Kv4<D>::block(P);
+    }
+    return st;
+}
+
+template <int D, int NC> struct Kv4State {
+    static constexpr int G = D / 32, DT = D / 16;
+    f32x4_t o[NC][DT];
+    float om[NC][G], m[NC], l[NC];
+
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int n = 0; n < NC; n++) {
+#pragma unroll
+            for (int j = 0; j < DT; j++) o[n][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int g = 0; g < G; g++) om[n][g] = 0.f;
+            m[n] = -INFINITY; l[n] = 0.f;
+        }
+    }
+    // One step of 32 tokens from t0 on.  MASK: lim[n] is the number of tokens that the lane's column sees.
+    template <bool MASK>
+    __device__ __forceinline__ void step(const Kv4Query<D> (&x)[NC], const Kv4Keys<D> (&k)[2], const Kv4Values<D> (&v)[2], const int (&lim)[NC],
+                                         const Kv4Step &st, int t0, int q)
+    {
+#pragma clang fp contract(off)                      // (both instances of MASK round alike: a row's bits do not depend on which one it went through)
+        float z[NC][8], e[8];
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            f16x8_t kk[G];
+            k[i].widen(kk);
+#pragma unroll
+            for (int n = 0; n < NC; n++) {
+                const f32x4_t zz = k[i].scores(kk, x[n]);
+#pragma unroll
+                for (int j = 0; j < 4; j++) z[n][4 * i + j] = zz[j] * x[n].f;
+            }
+            float ee[4];
+            v[i].exponents(ee);
+#pragma unroll
+            for (int j = 0; j < 4; j++) e[4 * i + j] = ee[j];
+        }
+        uint32_t ph[NC][G][4], pl[NC][G][4];
+#pragma unroll
+        for (int n = 0; n < NC; n++) {
+            bool see[8];
+            float mx = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                see[j] = !MASK || (st.here[j >> 2] && t0 + 16 * (j >> 2) + 4 * q + (j & 3) < lim[n]);
+                if (!see[j]) z[n][j] = -INFINITY;
+                mx = fmaxf(mx, z[n][j] + e[j]);
+            }
+            mx = quads_max(mx);
+            if (__any(mx > m[n])) {                 // (where it stays the factor is 1)
+                const float m_new = fmaxf(m[n], mx), alpha = __builtin_amdgcn_exp2f(m[n] - (m_new == -INFINITY ? 0.f : m_new));
+#pragma unroll
+                for (int j = 0; j < DT; j++) o[n][j] *= alpha;
+#pragma unroll
+                for (int g = 0; g < G; g++) om[n][g] *= alpha;
+                l[n] *= alpha;
+                m[n] = m_new;
+            }
+            const float ref = (m[n] == -INFINITY ? 0.f : m[n]) - 14.f;
+            float p[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                p[j] = __builtin_amdgcn_exp2f(z[n][j] - ref);
+                l[n] += p[j];
+            }
+#pragma unroll
+            for (int g = 0; g < G; g++)
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {
+                    const uint32_t sw = v[j >> 2].s[2 * g + (j >> 1 & 1)], mw = v[j >> 2].m[2 * g + (j >> 1 & 1)];
+                    const float x0 = see[j] ? p[j] * half_of(sw, 0) : 0.f, x1 = see[j + 1] ? p[j + 1] * half_of(sw, 1) : 0.f;
+                    kv4_split(x0, x1, ph[n][g][j >> 1], pl[n][g][j >> 1]);
+                    if (see[j]) om[n][g] = fmaf(p[j], half_of(mw, 0), om[n][g]);
+                    if (see[j + 1]) om[n][g] = fmaf(p[j + 1], half_of(mw, 1), om[n][g]);
+                }
+        }
+        constexpr int VH = D / 64;
+#pragma unroll
+        for (int h = 0; h < VH; h++) {
+            uint32_t u[4][4];
+#pragma unroll
+            for (int a = 0; a < 4; a++) kv4_widen(v[a >> 1].w[2 * h + (a & 1)], u[a]);
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                // nibble i of a word's halves; kv4_widen numbers the nibbles of a half 0, 1, 2, 3
+                Kv4Op a;
+#pragma unroll
+                for (int w = 0; w < 4; w++) a.w[w] = u[w][i];
+                const int j = 4 * h + i;
+#pragma unroll
+                for (int n = 0; n < NC; n++) {
+                    Kv4Op hi, lo;
+#pragma unroll
+                    for (int w = 0; w < 4; w++) { hi.w[w] = ph[n][j >> 1][w]; lo.w[w] = pl[n][j >> 1][w]; }
+                    o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, hi.v, o[n][j], 0, 0, 0);
+                    o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, lo.v, o[n][j], 0, 0, 0);
+                }
+            }
+        }
+    }
+    // the minima's part joins the sums, the lanes of a column their parts of the probabilities' sum
+    __device__ __forceinline__ void finish()
+    {
+#pragma unroll
+        for (int n = 0; n < NC; n++) {
+            l[n] = quads_sum(l[n]);
+#pragma unroll
+            for (int g = 0; g < G; g++) om[n][g] = quads_sum(om[n][g]);
+#pragma unroll
+            for (int j = 0; j < DT; j++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) o[n][j][i] += om[n][j >> 1];
+        }
+    }
+};
+
+// steps t0, t0 + stride, .. below t1 of the columns x
+template <int D, int NC>
+__device__ __forceinline__ void kv4_run(const Kv4View &c, int s, int h, Kv4State<D, NC> &state, const Kv4Query<D> (&x)[NC], const int (&lim)[NC], int least,
+                                        int t0, int t1, int stride, int lane)
+{
+    const int P = 1 << c.logT, q = lane >> 4;
+    for (int t = t0; t < t1; t += stride) {
+        const Kv4Step st = kv4_step<D>(c, s, h, t, t1);
+        Kv4Keys<D> k[2];
+        Kv4Values<D> v[2];
+#pragma unroll
+        for (int i = 0; i < 2; i++) k[i].load(st.blk[i], P, st.t[i], lane);
+#pragma unroll
+        for (int i = 0; i < 2; i++) v[i].load(st.blk[i], P, st.t[i], lane);
+        if (t + 32 <= least && st.here[0] && st.here[1]) state.template step<false>(x, k, v, lim, st, t, q);
+        else state.template step<true>(x, k, v, lim, st, t, q);
+    }
+}
+
+// what a lane's column is: row and head, tokens it sees (0: a column behind the sequence's last)
+struct Kv4Column { int row, head, lim; };
+__device__ __forceinline__ Kv4Column kv4_column(const Kv4Attn &a, const Kv4Cols &k, int h, int col, int len)
+{
+    Kv4Column c;
+    const bool live = col < k.n;
+    const int i = live ? col : 0;
+    c.row = k.r0 + i / a.group;
+    c.head = h * a.group + i % a.group;
+    c.lim = live ? max(0, min(len - k.end + c.row + 1, a.max_len)) : 0;
+    return c;
+}
+__device__ __forceinline__ int lanes_min(int v)
+{
+    for (int o = 1; o < 16; o <<= 1) v = min(v, __shfl_xor(v, o));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int lanes_max(int v)
+{
+    for (int o = 1; o < 16; o <<= 1) v = max(v, __shfl_xor(v, o));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+
+// outputs d = 16 j + 4 q + 0..3 of a row, from sums over l
+template <typename T> __device__ __forceinline__ void kv4_store4(T *p, bool aligned, f32x4_t v)
+{
+    if (aligned) {
+        typedef T vec_t __attribute__((ext_vector_type(4)));
+        *(vec_t *)p = vec_t{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) p[i] = (T)v[i];
+    }
+}
+
+// Few columns: a workgroup takes a chunk of the tokens for one cache head and up to 16 columns, its four waves every fourth step.
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void kv4_attend_few_kernel(const Kv4Attn a)
+{
+    constexpr int DT = D / 16;
+    __shared__ float os[4][16][D + 4], ms[4][16], ls[4][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4, h = blockIdx.y, chunk = blockIdx.z;
+    const Kv4Cols k = kv4_columns<16>(a, blockIdx.x);
+    if (k.s < 0) return;
+    const int len = kv4_len(a.c, k.s);
+    const Kv4Column col = kv4_column(a, k, h, k.c0 + (lane & 15), len);
+    const bool live = k.c0 + (lane & 15) < k.n;
+    const int lim[1] = {col.lim};
+    const int most = lanes_max(col.lim), least = lanes_min(live ? col.lim : 1 << 30);
+    const int t0 = chunk * a.chunk, t1 = min(most, t0 + a.chunk);
+    if (t0 >= t1 && chunk > 0) return;                    // the merge knows from the rows' places
+    Kv4Query<D> x[1];
+    const T *row = (const T *)a.q + (size_t)col.row * a.q_stride + (size_t)col.head * D;
+    x[0].load(row, live, ((uintptr_t)a.q | (uintptr_t)a.q_stride * sizeof(T)) % (8 * sizeof(T)) == 0, a.scale, q);
+    Kv4State<D, 1> state;
+    state.clear();
+    kv4_run<D, 1>(a.c, k.s, h, state, x, lim, least, t0 + 32 * wave, t1, 128, lane);
+    state.finish();
+    if (q == 0) { ms[wave][lane] = state.m[0]; ls[wave][lane] = state.l[0]; }
+#pragma unroll
+    for (int j = 0; j < DT; j++) *(f32x4_t *)&os[wave][lane & 15][16 * j + 4 * q] = state.o[0][j];
+    __syncthreads();
+    // a thread takes four outputs of a column
+    for (int i = threadIdx.x; i < 16 * (D / 4); i += 256) {
+        const int cc = i / (D / 4), d = i % (D / 4) * 4;
+        if (k.c0 + cc >= k.n) continue;
+        const Kv4Column kc = kv4_column(a, k, h, k.c0 + cc, len);
+        float m = ms[0][cc];
+        for (int w = 1; w < 4; w++) m = fmaxf(m, ms[w][cc]);
+        const float ref = m == -INFINITY ? 0.f : m;
+        float l = 0.f;
+        f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < 4; w++) {
+            const float f = __builtin_amdgcn_exp2f(ms[w][cc] - ref);
+            l = fmaf(f, ls[w][cc], l);
+            const f32x4_t ow = *(const f32x4_t *)&os[w][cc][d];
+            for (int e = 0; e < 4; e++) o[e] = fmaf(f, ow[e], o[e]);
+        }
+        if (a.n_chunks > 1) {
+            float *p = a.part + (((size_t)chunk * a.n_rows + kc.row) * a.heads + kc.head) * (D + 2);
+            for (int e = 0; e < 4; e++) p[d + e] = o[e];
+            if (d == 0) { p[D] = m; p[D + 1] = l; }
+        } else {
+            for (int e = 0; e < 4; e++) o[e] = l == 0.f ? 0.f : o[e] / l;
+            kv4_store4((T *)a.out + (size_t)kc.row * a.out_stride + (size_t)kc.head * D + d,
+                       ((uintptr_t)a.out | (uintptr_t)a.out_stride * sizeof(T)) % (4 * sizeof(T)) == 0, o);
+            if (d == 0) a.lse[(size_t)kc.row * a.heads + kc.head] = l == 0.f ? -INFINITY : m - 14.f + __builtin_amdgcn_logf(l);
+        }
+    }
+}
+
+// Many columns (prompt rows): a wave takes 16 NC columns over all tokens of a chunk; the four waves of a workgroup read the same tokens
+// at about the same time.
+template <typename T, int D, int NC>
+__global__ __launch_bounds__(256, 1) void kv4_attend_many_kernel(const Kv4Attn a)
+{
+    constexpr int DT = D / 16;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4, h = blockIdx.y, chunk = blockIdx.z;
+    const Kv4Cols k = kv4_columns<64 * NC>(a, blockIdx.x);
+    if (k.s < 0) return;
+    const int len = kv4_len(a.c, k.s), c0 = k.c0 + __builtin_amdgcn_readfirstlane(wave) * 16 * NC;
+    if (c0 >= k.n) return;
+    Kv4Query<D> x[NC];
+    int lim[NC], most = 0, least = 1 << 30;
+    Kv4Column col[NC];
+#pragma unroll
+    for (int n = 0; n < NC; n++) {
+        const int cc = c0 + 16 * n + (lane & 15);
+        const bool live = cc < k.n;
+        col[n] = kv4_column(a, k, h, cc, len);
+        lim[n] = col[n].lim;
+        most = max(most, lanes_max(lim[n])); least = min(least, lanes_min(live ? lim[n] : 1 << 30));
+        const T *row = (const T *)a.q + (size_t)col[n].row * a.q_stride + (size_t)col[n].head * D;
+        x[n].load(row, live, ((uintptr_t)a.q | (uintptr_t)a.q_stride * sizeof(T)) % (8 * sizeof(T)) == 0, a.scale, q);
+    }
+    const int t0 = chunk * a.chunk, t1 = min(most, t0 + a.chunk);
+    if (t0 >= t1 && chunk > 0) return;
+    Kv4State<D, NC> state;
+    state.clear();
+    kv4_run<D, NC>(a.c, k.s, h, state, x, lim, least, t0, t1, 32, lane);
+    state.finish();
+    const bool aligned = ((uintptr_t)a.out | (uintptr_t)a.out_stride * sizeof(T)) % (4 * sizeof(T)) == 0;
+#pragma unroll
+    for (int n = 0; n < NC; n++) {
+        if (c0 + 16 * n + (lane & 15) >= k.n) continue;
+        const float l = state.l[n];
+        if (a.n_chunks > 1) {
+            float *p = a.part + (((size_t)chunk * a.n_rows + col[n].row) * a.heads + col[n].head) * (D + 2);
+#pragma unroll
+            for (int j = 0; j < DT; j++)
+                for (int i = 0; i < 4; i++) p[16 * j + 4 * q + i] = state.o[n][j][i];
+            if (q == 0) { p[D] = state.m[n]; p[D + 1] = l; }
+        } else {
+            T *out = (T *)a.out + (size_t)col[n].row * a.out_stride + (size_t)col[n].head * D;
+#pragma unroll
+            for (int j = 0; j < DT; j++) {
+                f32x4_t o;
+                for (int i = 0; i < 4; i++) o[i] = l == 0.f ? 0.f : state.o[n][j][i] / l;
+                kv4_store4(out + 16 * j + 4 * q, aligned, o);
+            }
+            if (q == 0) a.lse[(size_t)col[n].row * a.heads + col[n].head] = l == 0.f ? -INFINITY : state.m[n] - 14.f + __builtin_amdgcn_logf(l);
+        }
+    }
+}
+
+// Joins the chunks of a row and head: a wave each.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void kv4_join_kernel(const Kv4Attn a)
+{
+    const int lane = threadIdx.x & 63;
+    const size_t item = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (item >= (size_t)a.n_rows * a.heads) return;
+    const int r = (int)(item / a.heads), hq = (int)(item % a.heads);
+    const Kv4Row row = kv4_row(a.c, a.row_start, r);
+    if (row.s < 0) return;
+    // Chunks behind the last token that any column of the row's block sees were not written.  They end no earlier than the row's own.
+    const int lim = max(0, min(row.pos + 1, a.max_len)), n = max(1, (lim + a.chunk - 1) / a.chunk);
+    const float *p = a.part + ((size_t)r * a.heads + hq) * (D + 2);
+    const size_t step = (size_t)a.n_rows * a.heads * (D + 2);
+    float m = -INFINITY;
+    for (int i = 0; i < n; i++) m = fmaxf(m, p[i * step + D]);
+    const float ref = m == -INFINITY ? 0.f : m;
+    float l = 0.f, o[D / 64] = {};
+    for (int i = 0; i < n; i++) {
+        const float f = __builtin_amdgcn_exp2f(p[i * step + D] - ref);
+        l = fmaf(f, p[i * step + D + 1], l);
+#pragma unroll
+        for (int e = 0; e < D / 64; e++) o[e] = fmaf(f, p[i * step + lane + 64 * e], o[e]);
+    }
+    T *out = (T *)a.out + (size_t)r * a.out_stride + (size_t)hq * D;
+#pragma unroll
+    for (int e = 0; e < D / 64; e++) out[lane + 64 * e] = (T)(l == 0.f ? 0.f : o[e] / l);
+    if (lane == 0) a.lse[(size_t)r * a.heads + hq] = l == 0.f ? -INFINITY : m - 14.f + __builtin_amdgcn_logf(l);
+}
+
+// w_out[s][h][t] = w_in + the probabilities of token t, summed over the rows and the query heads of head h.  A wave takes 32 tokens and goes over
+// all columns; a column's scores are those of the attention, its probabilities 2^(z - lse).
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void kv4_weights_kernel(const Kv4Attn a)
+{
+    constexpr int G = D / 32;
+    const int s = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 63, q = lane >> 4, P = 1 << a.c.logT;
+    const int t0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * 32;
+    const int len = kv4_len(a.c, s), n = min(len, a.max_len);
+    if (t0 >= n) return;
+    Kv4Cols k;
+    k.s = s; k.c0 = 0;
+    k.r0 = min(max(a.row_start[s], 0), a.n_rows); k.end = a.row_start[s + 1];
+    k.n = (min(max(k.end, k.r0), a.n_rows) - k.r0) * a.group;
+    const Kv4Step st = kv4_step<D>(a.c, s, h, t0, n);
+    Kv4Keys<D> keys[2];
+    f16x8_t kk[2][G];
+#pragma unroll
+    for (int i = 0; i < 2; i++) { keys[i].load(st.blk[i], P, st.t[i], lane); keys[i].widen(kk[i]); }
+    float sum[8] = {};
+    const bool aligned = ((uintptr_t)a.q | (uintptr_t)a.q_stride * sizeof(T)) % (8 * sizeof(T)) == 0;
+    // columns in front of the first that sees token t0 see none of these
+    int first = t0 - (len - k.end + k.r0);
+    first = first > 0 && t0 < n ? min(first, k.n) * a.group : 0;
+    for (int c0 = min(first, k.n) & ~15; c0 < k.n; c0 += 16) {
+        const Kv4Column col = kv4_column(a, k, h, c0 + (lane & 15), len);
+        const bool live = c0 + (lane & 15) < k.n;
+        Kv4Query<D> x;
+        x.load((const T *)a.q + (size_t)col.row * a.q_stride + (size_t)col.head * D, live, aligned, a.scale, q);
+        const float lse = live ? a.lse[(size_t)col.row * a.heads + col.head] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const f32x4_t z = keys[i].scores(kk[i], x);
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+                if (st.here[i] && t0 + 16 * i + 4 * q + j < col.lim) sum[4 * i + j] += __builtin_amdgcn_exp2f(z[j] * x.f - lse);
+        }
+    }
+    // over the 16 columns of a tile
+#pragma unroll
+    for (int j = 0; j < 8; j++)
+        for (int o = 1; o < 16; o <<= 1) sum[j] += __shfl_xor(sum[j], o);
+    const size_t at = ((size_t)s * a.c.H + h) * ((size_t)a.c.max_pages << a.c.logT);
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        const int t = t0 + 16 * (j >> 2) + 4 * q + (j & 3);
+        if ((lane & 15) == j && t < n) a.w_out[at + t] = (a.w_in ? a.w_in[at + t] : 0.f) + sum[j];
+    }
 }
 
 // ---- eviction -----------------------------------------------------------------------------------
