@@ -501,37 +501,39 @@ class Kv4Cache:
         n_pages = (pool.numel() + stride - need) // stride
         if n_pages < 1 or n_seqs < 1 or max_pages < 1 or lens.shape[0] != n_seqs:
             raise ValueError("the pool holds no page, the page table is empty, or lens does not fit it")
-        self.pool, self.page_table, self.lens, self.device = pool, page_table, lens, pool.device
+        self.pool, self.page_table, self.lens, self.device, self.index = pool, page_table, lens, pool.device, pool.device.index
+        self._codes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
         self.n_seqs, self.max_pages, self.n_pages = n_seqs, max_pages, n_pages
         self.n_kv_heads, self.head_dim, self.page_tokens, self.page_stride = n_kv_heads, head_dim, page_tokens, stride
         self.capacity = max_pages * page_tokens
         self.c = kg_kv4_cache(pool.data_ptr(), stride, n_pages, page_tokens, n_kv_heads, head_dim, n_seqs, max_pages,
                               page_table.data_ptr(), lens.data_ptr())
 
-    def _call(self, name, *args):
-        """The library's call on the current stream of the cache's GPU."""
-        cuda, fn = self._torch.cuda, getattr(self.L, name)
-        stream = cuda.current_stream(self.device).cuda_stream
-        if cuda.current_device() == self.device.index:
+    def _call(self, fn, *args):
+        """The library's call on the current stream of the cache's GPU.  (The stream's handle is asked for without a Stream object around
+        it, which costs 2 us of the 5 that a call of one small launch takes.)"""
+        cuda = self._torch.cuda
+        stream = self._torch._C._cuda_getCurrentRawStream(self.index)
+        if cuda.current_device() == self.index:
             rc = fn(*args, stream)
         else:
             with cuda.device(self.device):
                 rc = fn(*args, stream)
         if rc != KG_OK:
-            raise KangarooError(rc, name)
+            raise KangarooError(rc, fn.__name__)
 
     def _rows(self, t, heads, name):
-        """(dtype code, address, row stride) of rows [n][heads][head_dim]."""
-        torch = self._torch
-        code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(t.dtype)
-        if code is None or t.dim() != 3 or t.shape[2] != self.head_dim or (heads and t.shape[1] != heads) or t.device != self.device:
+        """(dtype code, address, row stride, rows, heads) of rows [n][heads][head_dim]."""
+        code, shape = self._codes.get(t.dtype), t.shape
+        if code is None or len(shape) != 3 or shape[2] != self.head_dim or (heads and shape[1] != heads) or t.device != self.device:
             raise ValueError(f"{name}: rows [n][{heads or 'heads'}][{self.head_dim}] of float32, bfloat16 or float16 on {self.device} wanted")
-        if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != self.head_dim):
+        stride = t.stride()
+        if stride[2] != 1 or (stride[1] != self.head_dim and shape[1] > 1):
             raise ValueError(f"{name}: the heads of a row have to lie together")
-        return code, t.data_ptr(), t.stride(0)
+        return code, t.data_ptr(), stride[0], shape[0], shape[1]
 
     def _starts(self, row_start):
-        if row_start.dtype != self._torch.int32 or row_start.shape != (self.n_seqs + 1,) or not row_start.is_contiguous() or row_start.device != self.device:
+        if row_start.dtype is not self._torch.int32 or row_start.shape != (self.n_seqs + 1,) or not row_start.is_contiguous() or row_start.device != self.device:
             raise ValueError(f"row_start has to be an int32 tensor of {self.n_seqs + 1} entries on {self.device}")
         return row_start.data_ptr()
 
@@ -543,22 +545,22 @@ class Kv4Cache:
         return t.data_ptr()
 
 
+def _kv4_pair(cache: Kv4Cache, fn, k, v, row_start) -> None:
+    dt, kp, ks, n, _ = cache._rows(k, cache.n_kv_heads, "k")
+    dv, vp, vs, nv, _ = cache._rows(v, cache.n_kv_heads, "v")
+    if dt != dv or n != nv:
+        raise ValueError("k and v differ in type or number of rows")
+    cache._call(fn, cache.c, dt, kp, ks, vp, vs, cache._starts(row_start), n)
+
+
 def op_kv4_append(cache: Kv4Cache, k, v, row_start) -> None:
     """Stores rows k, v [n][n_kv_heads][head_dim] as the last tokens of their sequences (kg_op_kv4_append)."""
-    dt, kp, ks = cache._rows(k, cache.n_kv_heads, "k")
-    dv, vp, vs = cache._rows(v, cache.n_kv_heads, "v")
-    if dt != dv or k.shape[0] != v.shape[0]:
-        raise ValueError("k and v differ in type or number of rows")
-    cache._call("kg_op_kv4_append", cache.c, dt, kp, ks, vp, vs, cache._starts(row_start), k.shape[0])
+    _kv4_pair(cache, cache.L.kg_op_kv4_append, k, v, row_start)
 
 
 def op_kv4_read(cache: Kv4Cache, row_start, k, v) -> None:
     """Fills rows k, v with what the cache holds for the last tokens of the sequences (kg_op_kv4_read)."""
-    dt, kp, ks = cache._rows(k, cache.n_kv_heads, "k")
-    dv, vp, vs = cache._rows(v, cache.n_kv_heads, "v")
-    if dt != dv or k.shape[0] != v.shape[0]:
-        raise ValueError("k and v differ in type or number of rows")
-    cache._call("kg_op_kv4_read", cache.c, dt, kp, ks, vp, vs, cache._starts(row_start), k.shape[0])
+    _kv4_pair(cache, cache.L.kg_op_kv4_read, k, v, row_start)
 
 
 def op_kv4_work_bytes(cache: Kv4Cache, n_rows: int, n_heads: int, max_len: int) -> int:
@@ -573,15 +575,15 @@ def op_kv4_attention(cache: Kv4Cache, q, row_start, out, max_len: int, work, sca
                      weights_out=None) -> None:
     """out = attention of the rows q [n][heads][head_dim] over the cache (kg_op_kv4_attention); scale: 1 / sqrt(head_dim) by default.
     weights_out [n_seqs][n_kv_heads][capacity] = weights_in plus each cached token's probability summed over rows and heads."""
-    dt, qp, qs = cache._rows(q, 0, "q")
-    do, op, os_ = cache._rows(out, q.shape[1], "out")
-    if dt != do or q.shape[0] != out.shape[0]:
+    dt, qp, qs, n, heads = cache._rows(q, 0, "q")
+    do, op, os_, no, _ = cache._rows(out, heads, "out")
+    if dt != do or n != no:
         raise ValueError("q and out differ in type or number of rows")
     if work.device != cache.device or not work.is_contiguous():
         raise ValueError(f"work has to be a contiguous tensor on {cache.device}")
-    cache._call("kg_op_kv4_attention", cache.c, dt, qp, qs, q.shape[1], cache._starts(row_start), q.shape[0], max_len,
+    cache._call(cache.L.kg_op_kv4_attention, cache.c, dt, qp, qs, heads, cache._starts(row_start), n, max_len,
                 cache.head_dim ** -0.5 if scale is None else scale, op, os_, cache._weights(weights_in, "weights_in"),
-                cache._weights(weights_out, "weights_out"), work.data_ptr(), work.numel() * work.element_size())
+                cache._weights(weights_out, "weights_out"), work.data_ptr(), work.nbytes)
 
 
 def op_kv4_evict(src: Kv4Cache, dst: Kv4Cache, n_keep: int, n_first: int, n_recent: int, weights_in, weights_out, kept) -> None:
@@ -595,5 +597,5 @@ def op_kv4_evict(src: Kv4Cache, dst: Kv4Cache, n_keep: int, n_first: int, n_rece
         raise ValueError("evict needs weights_in and weights_out")
     if src.n_seqs != dst.n_seqs or src.n_kv_heads != dst.n_kv_heads or src.head_dim != dst.head_dim:
         raise ValueError("src and dst differ in sequences or heads")
-    src._call("kg_op_kv4_evict", src.c, dst.c, n_keep, n_first, n_recent, src._weights(weights_in, "weights_in"),
+    src._call(src.L.kg_op_kv4_evict, src.c, dst.c, n_keep, n_first, n_recent, src._weights(weights_in, "weights_in"),
               dst._weights(weights_out, "weights_out"), kept.data_ptr())

@@ -2564,9 +2564,7 @@ int kg_op_kv4_append(const kg_kv4_cache *c, int dtype, const void *k, long k_str
     const long w = (long)c->n_kv_heads * c->head_dim;
     if (!kv4_rows_ok(k, k_stride, w, n_rows, esz) || !kv4_rows_ok(v, v_stride, w, n_rows, esz)) return KG_EINVAL;
     const Kv4View view = kv4_view(c);
-    const size_t lanes = (size_t)n_rows * c->n_kv_heads * (c->head_dim / 8);
-    if (lanes > (size_t)255 << 31) return KG_EINVAL;
-    const dim3 grid((unsigned)((lanes + 255) / 256));
+    const dim3 grid((unsigned)(((size_t)n_rows * (c->head_dim / 8) + 255) / 256), c->n_kv_heads);
 #define KV4_LAUNCH(T, D) \
     hipLaunchKernelGGL((kv4_append_kernel<T, D>), grid, dim3(256), 0, (hipStream_t)hip_stream, view, (const T *)k, k_stride, (const T *)v, v_stride, row_start, n_rows)
     KV4_BY_TYPE_AND_DIM(KV4_LAUNCH, c->head_dim);
@@ -2584,9 +2582,7 @@ int kg_op_kv4_read(const kg_kv4_cache *c, int dtype, void *k, long k_stride, voi
     if (!kv4_rows_ok(k, k_stride, w, n_rows, esz) || !kv4_rows_ok(v, v_stride, w, n_rows, esz)) return KG_EINVAL;
     if (kv4_rows_share(k, k_stride, v, v_stride, w, n_rows, esz)) return KG_EINVAL;
     const Kv4View view = kv4_view(c);
-    const size_t lanes = (size_t)n_rows * c->n_kv_heads * (c->head_dim / 8);
-    if (lanes > (size_t)255 << 31) return KG_EINVAL;
-    const dim3 grid((unsigned)((lanes + 255) / 256));
+    const dim3 grid((unsigned)(((size_t)n_rows * (c->head_dim / 8) + 255) / 256), c->n_kv_heads);
 #define KV4_LAUNCH(T, D) \
     hipLaunchKernelGGL((kv4_read_kernel<T, D>), grid, dim3(256), 0, (hipStream_t)hip_stream, view, (T *)k, k_stride, (T *)v, v_stride, row_start, n_rows)
     KV4_BY_TYPE_AND_DIM(KV4_LAUNCH, c->head_dim);
@@ -2618,7 +2614,7 @@ static Kv4Plan kv4_plan(const kg_kv4_cache *c, int n_rows, int n_heads, int max_
     p.blocks = (int)std::min<long>(cols, (cols + cb - 1) / cb + std::min(c->n_seqs - 1, n_rows - 1));
     const int unit = 128, units = (len + unit - 1) / unit;
     const long per_chunk = (long)c->n_kv_heads * (p.few ? c->n_seqs : p.blocks), want = p.few ? 1024 : 512;
-    const long n = std::min<long>(units, std::max<long>(1, want / per_chunk));
+    const long n = std::min<long>({units, 256, std::max<long>(1, want / per_chunk)});      // (256: a lane of kv4_join_kernel each)
     p.chunk = (int)((units + n - 1) / n) * unit;
     p.n_chunks = (len + p.chunk - 1) / p.chunk;
     return p;
@@ -2630,7 +2626,7 @@ size_t kg_op_kv4_work_bytes(const kg_kv4_cache *c, int n_rows, int n_heads, int 
     if (n_rows == 0) return ALIGN;
     const Kv4Plan p = kv4_plan(c, n_rows, n_heads, max_len);
     const size_t lanes = (size_t)n_rows * n_heads;
-    return up(lanes * 4) + up(p.n_chunks > 1 ? lanes * p.n_chunks * (c->head_dim + 2) * 4 : 0);
+    return up(lanes * 4) + (p.n_chunks > 1 ? up(lanes * p.n_chunks * 8) + up(lanes * p.n_chunks * c->head_dim * 4) : 0);
 }
 
 int kg_op_kv4_attention(const kg_kv4_cache *c, int dtype, const void *q, long q_stride, int n_heads, const int32_t *row_start, int n_rows,
@@ -2653,15 +2649,17 @@ int kg_op_kv4_attention(const kg_kv4_cache *c, int dtype, const void *q, long q_
     a.c = kv4_view(c); a.q = q; a.out = out; a.q_stride = q_stride; a.out_stride = out_stride; a.row_start = row_start; a.n_rows = n_rows;
     a.heads = n_heads; a.group = n_heads / c->n_kv_heads; a.max_len = (int)std::min<size_t>(max_len, cap); a.scale = scale;
     a.w_in = weights_in; a.w_out = weights_out; a.lse = (float *)work;
-    a.part = (float *)((char *)work + up((size_t)n_rows * n_heads * 4));
     hipStream_t s = (hipStream_t)hip_stream;
     if (n_rows > 0) {
         const Kv4Plan p = kv4_plan(c, n_rows, n_heads, max_len);
+        const size_t lanes = (size_t)n_rows * n_heads;
         a.chunk = p.chunk; a.n_chunks = p.n_chunks;
+        a.part_ml = (float2 *)((char *)work + up(lanes * 4));
+        a.part = (float *)((char *)a.part_ml + up(lanes * p.n_chunks * 8));
         const dim3 grid(p.blocks, c->n_kv_heads, p.n_chunks);
 #define KV4_FEW(T, D) hipLaunchKernelGGL((kv4_attend_few_kernel<T, D>), grid, dim3(256), 0, s, a)
 #define KV4_MANY(T, D) hipLaunchKernelGGL((kv4_attend_many_kernel<T, D, KV4_MANY_TILES>), grid, dim3(256), 0, s, a)
-#define KV4_JOIN(T, D) hipLaunchKernelGGL((kv4_join_kernel<T, D>), dim3((unsigned)(((size_t)n_rows * n_heads + 3) / 4)), dim3(256), 0, s, a)
+#define KV4_JOIN(T, D) hipLaunchKernelGGL((kv4_join_kernel<T, D>), dim3((unsigned)lanes), dim3(256), 0, s, a)
         if (p.few) KV4_BY_TYPE_AND_DIM(KV4_FEW, c->head_dim);
         else KV4_BY_TYPE_AND_DIM(KV4_MANY, c->head_dim);
         if (p.n_chunks > 1) KV4_BY_TYPE_AND_DIM(KV4_JOIN, c->head_dim);

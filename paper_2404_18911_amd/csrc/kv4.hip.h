@@ -61,41 +61,84 @@ __device__ __forceinline__ Kv4Row kv4_row(const Kv4View &c, const int *row_start
     return {lo, kv4_len(c, lo) - row_start[lo + 1] + r};
 }
 
-template <typename T> __device__ __forceinline__ float row_ld(const T *p) { return (float)*p; }
+// eight elements of a row
+template <typename T> __device__ __forceinline__ void kv4_load8(const T *p, bool aligned, float (&x)[8])
+{
+    if (aligned) {
+        typedef T vec_t __attribute__((ext_vector_type(8)));
+        const vec_t v = *(const vec_t *)p;
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[e] = (float)v[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[e] = (float)p[e];
+    }
+}
+template <typename T> __device__ __forceinline__ void kv4_store8(T *p, bool aligned, const float (&x)[8])
+{
+    if (aligned) {
+        typedef T vec_t __attribute__((ext_vector_type(8)));
+        vec_t v;
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] = (T)x[e];
+        *(vec_t *)p = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) p[e] = (T)x[e];
+    }
+}
+// are the rows' pieces of n elements all aligned for one access
+template <typename T> __device__ __forceinline__ bool kv4_aligned(const void *p, long stride, int n)
+{
+    return (((uintptr_t)p | (uintptr_t)stride * sizeof(T)) & (n * sizeof(T) - 1)) == 0;
+}
 
 // The 16 levels of a group.  lo, hi: its least and largest component (clamped), bad: one of them is not finite.
-struct Kv4Levels { float s, m; };
+struct Kv4Levels { float s, m, r; };            // r: 1 / s, 0 where every level is 0
 __device__ __forceinline__ Kv4Levels kv4_levels(float lo, float hi, bool bad)
 {
     Kv4Levels l;
     l.m = bad ? 0.f : (float)(_Float16)lo;
     l.s = bad ? __builtin_nanf("") : (float)(_Float16)__fdiv_rn(__fsub_rn(hi, lo), 15.f);
+    l.r = l.s > 0.f ? __builtin_amdgcn_rcpf(l.s) : 0.f;
     return l;
 }
-// n = clamp(rint((x - m) / s), 0, 15) of the exact quotient: the rounded one of fp32 errs next to a border, so its residual is checked in 64 bits
+// n = clamp(rint((x - m) / s), 0, 15) of the exact quotient.  (x - m) r in fp32 is within 4e-6 of it (three roundings of a number below 16,
+// or beyond the last level), so only what comes as close as 1e-4 to a border is looked at again, in 64 bits, where x - m and n s are exact:
+// one in 5000, against 64 bits for all 65 us instead of 25 for a prompt's 4096 rows of 32 heads.
 __device__ __forceinline__ uint32_t kv4_level(float x, const Kv4Levels &l)
 {
-    if (!(l.s > 0.f)) return 0;
-    float n = fminf(fmaxf(rintf((x - l.m) / l.s), 0.f), 15.f);
-    const double s = l.s, rest = fma(-(double)n, s, (double)x - (double)l.m) * 2.0;
-    const bool odd = (int)n & 1;
-    if (rest > s || (rest == s && odd)) n += 1.f;
-    else if (rest < -s || (rest == -s && odd)) n -= 1.f;
-    return (uint32_t)fminf(fmaxf(n, 0.f), 15.f);
+    const float t = fminf(fmaxf((x - l.m) * l.r, 0.f), 15.f);
+    float n = rintf(t);
+    if (fabsf(t - n) > 0.4999f) {
+        const double s = l.s, rest = fma(-(double)n, s, (double)x - (double)l.m) * 2.0;
+        const bool odd = (int)n & 1;
+        if (rest > s || (rest == s && odd)) n += 1.f;
+        else if (rest < -s || (rest == -s && odd)) n -= 1.f;
+    }
+    return (uint32_t)n;
 }
 __device__ __forceinline__ float kv4_clamp(float x) { return fminf(fmaxf(x, -65504.f), 65504.f); }
 __device__ __forceinline__ bool kv4_bad(float x) { return !(fabsf(x) <= 3.402823466e38f); }
 
-// One row and head per D / 8 lanes, eight components each.
+// One row and head per D / 8 lanes, eight components each; a workgroup takes consecutive rows of one head, whose numbers lie together.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_append_kernel(const Kv4View c, const T *k, long k_stride, const T *v, long v_stride, const int *row_start,
                                                          int n_rows)
 {
     typedef Kv4<D> L;
     constexpr int LP = D / 8;
-    const int li = threadIdx.x & (LP - 1), lane = threadIdx.x & 63;
-    const size_t item = (size_t)blockIdx.x * (256 / LP) + threadIdx.x / LP;
-    const int r = (int)(item / c.H), h = (int)(item % c.H), P = 1 << c.logT;
+    const int li = threadIdx.x & (LP - 1), lane = threadIdx.x & 63, r = blockIdx.x * (256 / LP) + threadIdx.x / LP, h = blockIdx.y, P = 1 << c.logT;
+    float x[8], y[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) x[e] = y[e] = 0.f;
+    // values: component 16 j + i, lane li has i = li (D = 128: j = 0..7) or i = li, li + 8 (D = 64: j = 0..3 each)
+    if (r < n_rows) {
+        kv4_load8(k + (size_t)r * k_stride + (size_t)h * D + 8 * li, kv4_aligned<T>(k, k_stride, 8), x);
+        const T *row = v + (size_t)r * v_stride + (size_t)h * D + li;
+#pragma unroll
+        for (int e = 0; e < 8; e++) y[e] = (float)row[D == 128 ? 16 * e : 16 * (e & 3) + 8 * (e >> 2)];
+    }
     char *blk = nullptr;
     int t = 0;
     if (r < n_rows) {
@@ -108,17 +151,19 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(const Kv4View c, const 
     const bool live = blk != nullptr;
     {
         const int g = li >> 2, q = li & 3;
-        float x[8], lo = INFINITY, hi = -INFINITY;
+        float lo = INFINITY, hi = -INFINITY;
         bool bad = false;
+#pragma unroll
         for (int e = 0; e < 8; e++) {
-            x[e] = live ? row_ld(k + (size_t)r * k_stride + (size_t)h * D + 32 * g + 8 * q + e) : 0.f;
             bad |= kv4_bad(x[e]);
             x[e] = kv4_clamp(x[e]);
             lo = fminf(lo, x[e]); hi = fmaxf(hi, x[e]);
         }
-        for (int o = 1; o < 4; o <<= 1) { lo = fminf(lo, __shfl_xor(lo, o)); hi = fmaxf(hi, __shfl_xor(hi, o)); }
+        lo = fminf(lo, quad_x1(lo)); hi = fmaxf(hi, quad_x1(hi));
+        lo = fminf(lo, quad_x2(lo)); hi = fmaxf(hi, quad_x2(hi));
         const Kv4Levels l = kv4_levels(lo, hi, (__ballot(bad) >> (lane & ~3)) & 15);
         uint32_t w = 0;
+#pragma unroll
         for (int e = 0; e < 8; e++) w |= kv4_level(x[e], l) << (4 * e);
         if (live) {
             *(uint32_t *)(blk + L::k_word(P, t, q, g)) = w;
@@ -128,30 +173,33 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(const Kv4View c, const 
             }
         }
     }
-    // values: component 16 j + r, lane li has r = li (D = 128: j = 0..7) or r = li, li + 8 (D = 64: j = 0..3 each)
-    float x[8];
     bool bad[8];
+#pragma unroll
     for (int e = 0; e < 8; e++) {
-        const int d = D == 128 ? 16 * e + li : 16 * (e & 3) + li + 8 * (e >> 2);
-        x[e] = live ? row_ld(v + (size_t)r * v_stride + (size_t)h * D + d) : 0.f;
-        bad[e] = kv4_bad(x[e]);
-        x[e] = kv4_clamp(x[e]);
+        bad[e] = kv4_bad(y[e]);
+        y[e] = kv4_clamp(y[e]);
     }
     uint32_t w[2] = {0, 0};
+#pragma unroll
     for (int g = 0; g < L::G; g++) {
         // the elements of group g: j = 2 g, 2 g + 1
         float lo = INFINITY, hi = -INFINITY;
         bool b = false;
+#pragma unroll
         for (int e = 0; e < 8; e++) {
             if ((D == 128 ? e : e & 3) >> 1 != g) continue;
-            lo = fminf(lo, x[e]); hi = fmaxf(hi, x[e]);
+            lo = fminf(lo, y[e]); hi = fmaxf(hi, y[e]);
             b |= bad[e];
         }
-        for (int o = 1; o < LP; o <<= 1) { lo = fminf(lo, __shfl_xor(lo, o)); hi = fmaxf(hi, __shfl_xor(hi, o)); }
+        lo = fminf(lo, quad_x1(lo)); hi = fmaxf(hi, quad_x1(hi));
+        lo = fminf(lo, quad_x2(lo)); hi = fmaxf(hi, quad_x2(hi));
+        lo = fminf(lo, half_mirror(lo)); hi = fmaxf(hi, half_mirror(hi));
+        if (LP == 16) { lo = fminf(lo, row_mirror(lo)); hi = fmaxf(hi, row_mirror(hi)); }
         const Kv4Levels l = kv4_levels(lo, hi, (__ballot(b) >> (lane & ~(LP - 1))) & ((1ull << LP) - 1));
+#pragma unroll
         for (int e = 0; e < 8; e++) {
             if ((D == 128 ? e : e & 3) >> 1 != g) continue;
-            w[e >> 2] |= kv4_level(x[e], l) << (4 * (e & 3));
+            w[e >> 2] |= kv4_level(y[e], l) << (4 * (e & 3));
         }
         if (live && li == g) {
             *(_Float16 *)(blk + L::vs(P, t, g)) = (_Float16)l.s;
@@ -159,37 +207,38 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(const Kv4View c, const 
         }
     }
     if (live) {
+#pragma unroll
         for (int i = 0; i < 2; i++)
             *(uint16_t *)(blk + (D == 128 ? L::v_half(P, t, li, i) : L::v_half(P, t, li + 8 * i, 0))) = (uint16_t)w[i];
     }
 }
 
-// Keys and values of the rows, widened.  A token without a page reads as zeros.
+// Keys and values of the rows, widened.  A token without a page reads as zeros.  Eight components of a row and head per lane.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_read_kernel(const Kv4View c, T *k, long k_stride, T *v, long v_stride, const int *row_start, int n_rows)
 {
     typedef Kv4<D> L;
     constexpr int LP = D / 8;
-    const int li = threadIdx.x & (LP - 1);
-    const size_t item = (size_t)blockIdx.x * (256 / LP) + threadIdx.x / LP;
-    const int r = (int)(item / c.H), h = (int)(item % c.H), P = 1 << c.logT;
+    const int li = threadIdx.x & (LP - 1), r = blockIdx.x * (256 / LP) + threadIdx.x / LP, h = blockIdx.y, P = 1 << c.logT;
     if (r >= n_rows) return;
     const Kv4Row row = kv4_row(c, row_start, r);
     if (row.s < 0 || row.pos < 0) return;
     const char *blk = kv4_block<D>(c, row.s, h, row.pos);
-    const int t = row.pos & (P - 1);
-    for (int e = 0; e < 8; e++) {
-        const int d = 8 * li + e, g = d >> 5, j = d >> 4, rr = d & 15;
-        float kx = 0.f, vx = 0.f;
-        if (blk) {
-            const uint32_t kw = *(const uint32_t *)(blk + L::k_word(P, t, (d & 31) >> 3, g)) >> (4 * (d & 7)) & 15;
-            const uint32_t vw = *(const uint16_t *)(blk + L::v_half(P, t, rr, j >> 2)) >> (4 * (j & 3)) & 15;
-            kx = fmaf((float)*(const _Float16 *)(blk + L::ks(P, t, g)), (float)kw, (float)*(const _Float16 *)(blk + L::km(P, t, g)));
-            vx = fmaf((float)*(const _Float16 *)(blk + L::vs(P, t, g)), (float)vw, (float)*(const _Float16 *)(blk + L::vm(P, t, g)));
+    const int t = row.pos & (P - 1), g = li >> 2, j = li >> 1;
+    float kx[8] = {}, vx[8] = {};
+    if (blk) {
+        const uint32_t kw = *(const uint32_t *)(blk + L::k_word(P, t, li & 3, g));
+        const float ks = (float)*(const _Float16 *)(blk + L::ks(P, t, g)), km = (float)*(const _Float16 *)(blk + L::km(P, t, g));
+        const float vs = (float)*(const _Float16 *)(blk + L::vs(P, t, g)), vm = (float)*(const _Float16 *)(blk + L::vm(P, t, g));
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const uint32_t vw = *(const uint16_t *)(blk + L::v_half(P, t, 8 * (li & 1) + e, j >> 2));
+            kx[e] = fmaf(ks, (float)(kw >> (4 * e) & 15), km);
+            vx[e] = fmaf(vs, (float)(vw >> (4 * (j & 3)) & 15), vm);
         }
-        k[(size_t)r * k_stride + (size_t)h * D + d] = (T)kx;
-        v[(size_t)r * v_stride + (size_t)h * D + d] = (T)vx;
     }
+    kv4_store8(k + (size_t)r * k_stride + (size_t)h * D + 8 * li, kv4_aligned<T>(k, k_stride, 8), kx);
+    kv4_store8(v + (size_t)r * v_stride + (size_t)h * D + 8 * li, kv4_aligned<T>(v, v_stride, 8), vx);
 }
 
 // ---- attention ----------------------------------------------------------------------------------
@@ -198,8 +247,8 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(const Kv4View c, T *k, lo
 //   scores   z[t][c] = f_c (sum_g s_tg (n_t . q_c)_g + m_tg . (sum of q_c)_g): the levels n are exact in fp16, so a group's 32 products are one
 //            matrix instruction for each of two fp16 parts of the query (scaled by a power of two to below 2^10: the parts hold 22
 //            bits), its scale a multiplication in fp32; the minima are one more instruction over the groups, whose result the others add to.
-//   softmax  over steps with a running reference M_c, the largest z_t + e_t seen, e_t the exponent of the token's largest value scale:
-//            2^(z - M + 14) s is then below 2^14 whatever the sizes of values and scales, and as two fp16 parts is held to 22 bits
+//   softmax  over steps with a running reference M_c, the largest z_t + e_t seen, where the token's value scales are below 2^(e_t - 14):
+//            2^(z - M + 28) s is then below 2^14 whatever the sizes of values and scales, and as two fp16 parts is held to 22 bits
 //            and 2^-39 of the largest.
 //   values   o[d][c] = sum_t n_td (p_t s_tg)_c as matrix instructions, the levels again exact; sum_t p_t m_tg in fp32.
 // The scores of a lane (column lane % 16, tokens 4 (lane / 16) + 0..3 of both tiles) are the products' side of the second matrix
@@ -215,9 +264,11 @@ struct Kv4Attn {
     float scale;
     const float *w_in;
     float *w_out, *lse;                     // lse [row][head], base 2
-    float *part;                            // [n_chunks][row][head][D + 2]: sums, reference, sum of the probabilities
+    float *part;                            // [row][head][n_chunks][D]: a chunk's sums
+    float2 *part_ml;                        // [row][head][n_chunks]: their reference, sum of the probabilities
 };
 
+constexpr float KV4_SHIFT = 28.f;
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 union Kv4Op { uint32_t w[4]; f16x8_t v; };
 
@@ -232,27 +283,32 @@ __device__ __forceinline__ float quads_sum(float v)
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
-// levels i and i + 4 of a word as halves, i = 0..3
+// (w & mask) | bits in one instruction: the compiler makes two of it where both are constants
+__device__ __forceinline__ f16x2_t and_or(uint32_t w, uint32_t mask, uint32_t bits)
+{
+    uint32_t r;
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(w), "s"(mask), "v"(bits));
+    return __builtin_bit_cast(f16x2_t, r);
+}
+// levels i and i + 4 of a word as halves, i = 0..3: 1024 + n, or 1024 + 16 n of the nibble above, less what is too much
 __device__ __forceinline__ void kv4_widen(uint32_t w, uint32_t (&o)[4])
 {
     const f16x2_t one = {(_Float16)1024, (_Float16)1024}, sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f}, sixty_four = {(_Float16)64, (_Float16)64};
     const uint32_t hi = w >> 8;
-    // 1024 + n, or 1024 + 16 n of the nibble above
-    const f16x2_t a = __builtin_bit_cast(f16x2_t, (w & 0x000f000fu) | 0x64006400u), b = __builtin_bit_cast(f16x2_t, (w & 0x00f000f0u) | 0x64006400u);
-    const f16x2_t c = __builtin_bit_cast(f16x2_t, (hi & 0x000f000fu) | 0x64006400u), d = __builtin_bit_cast(f16x2_t, (hi & 0x00f000f0u) | 0x64006400u);
-    o[0] = __builtin_bit_cast(uint32_t, a - one);
-    o[1] = __builtin_bit_cast(uint32_t, b * sixteenth - sixty_four);
-    o[2] = __builtin_bit_cast(uint32_t, c - one);
-    o[3] = __builtin_bit_cast(uint32_t, d * sixteenth - sixty_four);
+    o[0] = __builtin_bit_cast(uint32_t, and_or(w, 0x000f000fu, 0x64006400u) - one);
+    o[1] = __builtin_bit_cast(uint32_t, and_or(w, 0x00f000f0u, 0x64006400u) * sixteenth - sixty_four);
+    o[2] = __builtin_bit_cast(uint32_t, and_or(hi, 0x000f000fu, 0x64006400u) - one);
+    o[3] = __builtin_bit_cast(uint32_t, and_or(hi, 0x00f000f0u, 0x64006400u) * sixteenth - sixty_four);
 }
 __device__ __forceinline__ float half_of(uint32_t w, int i) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(i ? w >> 16 : w)); }
 
 // two fp16 parts of a pair of numbers, rounded towards zero (the second takes what the first leaves)
 __device__ __forceinline__ void kv4_split(float x, float y, uint32_t &hi, uint32_t &lo)
 {
-#pragma clang fp contract(off)
+    float minus;                            // -1 in a register: x - (float)half as one mixed multiply-add, which the compiler would make a conversion and a difference
+    asm("v_mov_b32 %0, -1.0" : "=v"(minus));
     hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, y));
-    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x - half_of(hi, 0), y - half_of(hi, 1)));
+    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(fmaf(half_of(hi, 0), minus, x), fmaf(half_of(hi, 1), minus, y)));
 }
 
 // The columns of a block: sequence, first column, how many of the sequence's there are.
@@ -292,23 +348,9 @@ template <int CB> __device__ __forceinline__ Kv4Cols kv4_columns(const Kv4Attn &
     return {-1, 0, 0, 0, 0};
 }
 
-// eight elements of a row
-template <typename T> __device__ __forceinline__ void kv4_load8(const T *p, bool aligned, float (&x)[8])
-{
-    if (aligned) {
-        typedef T vec_t __attribute__((ext_vector_type(8)));
-        const vec_t v = *(const vec_t *)p;
-#pragma unroll
-        for (int e = 0; e < 8; e++) x[e] = (float)v[e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; e++) x[e] = (float)p[e];
-    }
-}
-
-// One column tile's queries: the products' side of the score instructions.
-template <int D> struct Kv4Query {
-    Kv4Op hi[D / 32], lo[D / 32], sum;      // slot 2 i, 2 i + 1 of lane group q: components 8 q + i, 8 q + i + 4 of the group
+// One column tile's queries: the products' side of the score instructions.  LO: the second part; 16-bit queries are exact without.
+template <int D, bool LO> struct Kv4Query {
+    Kv4Op hi[D / 32], lo[LO ? D / 32 : 1], sum;      // slot 2 i, 2 i + 1 of lane group q: components 8 q + i, 8 q + i + 4 of the group
     float f;                                // what a sum of products is worth as a base-2 exponent
 
     template <typename T> __device__ __forceinline__ void load(const T *row, bool live, bool aligned, float scale, int q)
@@ -334,7 +376,10 @@ template <int D> struct Kv4Query {
 #pragma unroll
             for (int e = 0; e < 8; e++) { x[g][e] = __builtin_amdgcn_ldexpf(x[g][e], 10 - ex); t += x[g][e]; }
 #pragma unroll
-            for (int i = 0; i < 4; i++) kv4_split(x[g][i], x[g][i + 4], hi[g].w[i], lo[g].w[i]);
+            for (int i = 0; i < 4; i++) {
+                if (LO) kv4_split(x[g][i], x[g][i + 4], hi[g].w[i], lo[LO ? g : 0].w[i]);
+                else hi[g].w[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x[g][i], x[g][i + 4]));
+            }
             total[g] = quads_sum(t);
         }
         kv4_split(total[0], total[1], sh[0], sl[0]);
@@ -349,12 +394,13 @@ template <int D> struct Kv4Keys {
     static constexpr int G = D / 32;
     uint32_t w[G], s[2 * G], m[G / 2];      // lane's token: words; tokens 4 q + 0..3: scales; lane's token: minima
 
+    // tile of tokens t.. of the page (t a multiple of 16); block and t are the wave's, the lane's part comes as 32-bit offsets
     __device__ __forceinline__ void load(const char *blk, int P, int t, int lane)
     {
-        const int q = lane >> 4, tok = t + (lane & 15);
-        __builtin_memcpy(w, __builtin_assume_aligned(blk + Kv4<D>::k_word(P, tok, q, 0), 4 * G), 4 * G);
-        __builtin_memcpy(s, __builtin_assume_aligned(blk + Kv4<D>::ks(P, t + 4 * q, 0), 16), 8 * G);
-        __builtin_memcpy(m, __builtin_assume_aligned(blk + Kv4<D>::km(P, tok, 0), 2 * G), 2 * G);
+        const uint32_t q = lane >> 4, tok = lane & 15;
+        __builtin_memcpy(w, __builtin_assume_aligned(blk + Kv4<D>::k_word(P, t, 0, 0) + (tok * (D / 2) + q * 4 * G), 4 * G), 4 * G);
+        __builtin_memcpy(s, __builtin_assume_aligned(blk + Kv4<D>::ks(P, t, 0) + q * 8 * G, 16), 8 * G);
+        __builtin_memcpy(m, __builtin_assume_aligned(blk + Kv4<D>::km(P, t, 0) + tok * 2 * G, 2 * G), 2 * G);
     }
     // the levels as the other side of the score instructions
     __device__ __forceinline__ void widen(f16x8_t (&k)[G]) const
@@ -367,7 +413,7 @@ template <int D> struct Kv4Keys {
         }
     }
     // scores of tokens 4 q + 0..3 in the units of Kv4Query::f
-    __device__ __forceinline__ f32x4_t scores(const f16x8_t (&k)[G], const Kv4Query<D> &x) const
+    template <bool LO> __device__ __forceinline__ f32x4_t scores(const f16x8_t (&k)[G], const Kv4Query<D, LO> &x) const
     {
         Kv4Op mm;
         mm.w[0] = mm.w[2] = m[0];
@@ -377,7 +423,7 @@ template <int D> struct Kv4Keys {
 #pragma unroll
         for (int g = 0; g < G; g++) {
             f32x4_t d = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[g], x.hi[g].v, zero, 0, 0, 0);
-            d = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[g], x.lo[g].v, d, 0, 0, 0);
+            if (LO) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[g], x.lo[LO ? g : 0].v, d, 0, 0, 0);
 #pragma unroll
             for (int i = 0; i < 4; i++) z[i] = fmaf(half_of(s[2 * g + (i >> 1)], i & 1), d[i], z[i]);
         }
@@ -390,24 +436,23 @@ template <int D> struct Kv4Values {
 
     __device__ __forceinline__ void load(const char *blk, int P, int t, int lane)
     {
-        const int q = lane >> 4;
-        __builtin_memcpy(w, __builtin_assume_aligned(blk + Kv4<D>::v_half(P, t + 4 * q, lane & 15, 0), 8 * VH), 8 * VH);
-        __builtin_memcpy(s, __builtin_assume_aligned(blk + Kv4<D>::vs(P, t + 4 * q, 0), 16), 8 * G);
-        __builtin_memcpy(m, __builtin_assume_aligned(blk + Kv4<D>::vm(P, t + 4 * q, 0), 16), 8 * G);
+        const uint32_t q = lane >> 4;
+        __builtin_memcpy(w, __builtin_assume_aligned(blk + Kv4<D>::v_half(P, t, 0, 0) + (uint32_t)lane * 8 * VH, 8 * VH), 8 * VH);
+        __builtin_memcpy(s, __builtin_assume_aligned(blk + Kv4<D>::vs(P, t, 0) + q * 8 * G, 16), 8 * G);
+        __builtin_memcpy(m, __builtin_assume_aligned(blk + Kv4<D>::vm(P, t, 0) + q * 8 * G, 16), 8 * G);
     }
-    // exponents of the tokens' largest scales (of garbage: some finite number)
+    // e of the tokens' largest scales, s < 2^(e - 14) (of garbage: 0..31).  Scales are not negative, so halves compare as whole numbers.
     __device__ __forceinline__ void exponents(float (&e)[4]) const
     {
+        typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
 #pragma unroll
         for (int a = 0; a < 2; a++) {
-            f16x2_t mx = __builtin_bit_cast(f16x2_t, s[a]);
+            u16x2_t mx = __builtin_bit_cast(u16x2_t, s[a]);
 #pragma unroll
-            for (int g = 1; g < G; g++) mx = __builtin_elementwise_max(mx, __builtin_bit_cast(f16x2_t, s[2 * g + a]));
-#pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const int ex = (int)(__builtin_bit_cast(uint32_t, mx) >> (16 * i + 10) & 31);      // s < 2^(ex - 14)
-                e[2 * a + i] = (float)(ex - 14);
-            }
+            for (int g = 1; g < G; g++) mx = __builtin_elementwise_max(mx, __builtin_bit_cast(u16x2_t, s[2 * g + a]));
+            const uint32_t w = __builtin_bit_cast(uint32_t, mx);
+            e[2 * a] = (float)(w >> 10 & 31);
+            e[2 * a + 1] = (float)(w >> 26 & 31);
         }
     }
 };
@@ -448,8 +493,8 @@ template <int D, int NC> struct Kv4State {
         }
     }
     // One step of 32 tokens from t0 on.  MASK: lim[n] is the number of tokens that the lane's column sees.
-    template <bool MASK>
-    __device__ __forceinline__ void step(const Kv4Query<D> (&x)[NC], const Kv4Keys<D> (&k)[2], const Kv4Values<D> (&v)[2], const int (&lim)[NC],
+    template <bool MASK, bool LO>
+    __device__ __forceinline__ void step(const Kv4Query<D, LO> (&x)[NC], const Kv4Keys<D> (&k)[2], const Kv4Values<D> (&v)[2], const int (&lim)[NC],
                                          const Kv4Step &st, int t0, int q)
     {
 #pragma clang fp contract(off)                      // (both instances of MASK round alike: a row's bits do not depend on which one it went through)
@@ -490,7 +535,7 @@ template <int D, int NC> struct Kv4State {
                 l[n] *= alpha;
                 m[n] = m_new;
             }
-            const float ref = (m[n] == -INFINITY ? 0.f : m[n]) - 14.f;
+            const float ref = (m[n] == -INFINITY ? 0.f : m[n]) - KV4_SHIFT;
             float p[8];
 #pragma unroll
             for (int j = 0; j < 8; j++) {
@@ -502,7 +547,7 @@ template <int D, int NC> struct Kv4State {
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {
                     const uint32_t sw = v[j >> 2].s[2 * g + (j >> 1 & 1)], mw = v[j >> 2].m[2 * g + (j >> 1 & 1)];
-                    const float x0 = see[j] ? p[j] * half_of(sw, 0) : 0.f, x1 = see[j + 1] ? p[j + 1] * half_of(sw, 1) : 0.f;
+                    const float x0 = see[j] ? fmaf(p[j], half_of(sw, 0), 0.f) : 0.f, x1 = see[j + 1] ? fmaf(p[j + 1], half_of(sw, 1), 0.f) : 0.f;
                     kv4_split(x0, x1, ph[n][g][j >> 1], pl[n][g][j >> 1]);
                     if (see[j]) om[n][g] = fmaf(p[j], half_of(mw, 0), om[n][g]);
                     if (see[j + 1]) om[n][g] = fmaf(p[j + 1], half_of(mw, 1), om[n][g]);
@@ -549,8 +594,8 @@ template <int D, int NC> struct Kv4State {
 };
 
 // steps t0, t0 + stride, .. below t1 of the columns x
-template <int D, int NC>
-__device__ __forceinline__ void kv4_run(const Kv4View &c, int s, int h, Kv4State<D, NC> &state, const Kv4Query<D> (&x)[NC], const int (&lim)[NC], int least,
+template <int D, int NC, bool LO>
+__device__ __forceinline__ void kv4_run(const Kv4View &c, int s, int h, Kv4State<D, NC> &state, const Kv4Query<D, LO> (&x)[NC], const int (&lim)[NC], int least,
                                         int t0, int t1, int stride, int lane)
 {
     const int P = 1 << c.logT, q = lane >> 4;
@@ -562,8 +607,8 @@ __device__ __forceinline__ void kv4_run(const Kv4View &c, int s, int h, Kv4State
         for (int i = 0; i < 2; i++) k[i].load(st.blk[i], P, st.t[i], lane);
 #pragma unroll
         for (int i = 0; i < 2; i++) v[i].load(st.blk[i], P, st.t[i], lane);
-        if (t + 32 <= least && st.here[0] && st.here[1]) state.template step<false>(x, k, v, lim, st, t, q);
-        else state.template step<true>(x, k, v, lim, st, t, q);
+        if (t + 32 <= least && st.here[0] && st.here[1]) state.template step<false, LO>(x, k, v, lim, st, t, q);
+        else state.template step<true, LO>(x, k, v, lim, st, t, q);
     }
 }
 
@@ -608,7 +653,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_few_kernel(const Kv4Attn a)
 {
     constexpr int DT = D / 16;
     __shared__ float os[4][16][D + 4], ms[4][16], ls[4][16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4, h = blockIdx.y, chunk = blockIdx.z;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, h = blockIdx.y, chunk = blockIdx.z;
     const Kv4Cols k = kv4_columns<16>(a, blockIdx.x);
     if (k.s < 0) return;
     const int len = kv4_len(a.c, k.s);
@@ -618,12 +663,12 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_few_kernel(const Kv4Attn a)
     const int most = lanes_max(col.lim), least = lanes_min(live ? col.lim : 1 << 30);
     const int t0 = chunk * a.chunk, t1 = min(most, t0 + a.chunk);
     if (t0 >= t1 && chunk > 0) return;                    // the merge knows from the rows' places
-    Kv4Query<D> x[1];
+    Kv4Query<D, sizeof(T) == 4> x[1];
     const T *row = (const T *)a.q + (size_t)col.row * a.q_stride + (size_t)col.head * D;
-    x[0].load(row, live, ((uintptr_t)a.q | (uintptr_t)a.q_stride * sizeof(T)) % (8 * sizeof(T)) == 0, a.scale, q);
+    x[0].load(row, live, kv4_aligned<T>(a.q, a.q_stride, 8), a.scale, q);
     Kv4State<D, 1> state;
     state.clear();
-    kv4_run<D, 1>(a.c, k.s, h, state, x, lim, least, t0 + 32 * wave, t1, 128, lane);
+    kv4_run(a.c, k.s, h, state, x, lim, least, t0 + 32 * wave, t1, 128, lane);
     state.finish();
     if (q == 0) { ms[wave][lane] = state.m[0]; ls[wave][lane] = state.l[0]; }
 #pragma unroll
@@ -646,14 +691,14 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_few_kernel(const Kv4Attn a)
             for (int e = 0; e < 4; e++) o[e] = fmaf(f, ow[e], o[e]);
         }
         if (a.n_chunks > 1) {
-            float *p = a.part + (((size_t)chunk * a.n_rows + kc.row) * a.heads + kc.head) * (D + 2);
-            for (int e = 0; e < 4; e++) p[d + e] = o[e];
-            if (d == 0) { p[D] = m; p[D + 1] = l; }
+            const size_t at = ((size_t)kc.row * a.heads + kc.head) * a.n_chunks + chunk;
+            *(f32x4_t *)(a.part + at * D + d) = o;
+            if (d == 0) a.part_ml[at] = float2{m, l};
         } else {
             for (int e = 0; e < 4; e++) o[e] = l == 0.f ? 0.f : o[e] / l;
             kv4_store4((T *)a.out + (size_t)kc.row * a.out_stride + (size_t)kc.head * D + d,
-                       ((uintptr_t)a.out | (uintptr_t)a.out_stride * sizeof(T)) % (4 * sizeof(T)) == 0, o);
-            if (d == 0) a.lse[(size_t)kc.row * a.heads + kc.head] = l == 0.f ? -INFINITY : m - 14.f + __builtin_amdgcn_logf(l);
+                       kv4_aligned<T>(a.out, a.out_stride, 4), o);
+            if (d == 0) a.lse[(size_t)kc.row * a.heads + kc.head] = l == 0.f ? -INFINITY : m - KV4_SHIFT + __builtin_amdgcn_logf(l);
         }
     }
 }
@@ -664,12 +709,12 @@ template <typename T, int D, int NC>
 __global__ __launch_bounds__(256, 1) void kv4_attend_many_kernel(const Kv4Attn a)
 {
     constexpr int DT = D / 16;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4, h = blockIdx.y, chunk = blockIdx.z;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, h = blockIdx.y, chunk = blockIdx.z;
     const Kv4Cols k = kv4_columns<64 * NC>(a, blockIdx.x);
     if (k.s < 0) return;
-    const int len = kv4_len(a.c, k.s), c0 = k.c0 + __builtin_amdgcn_readfirstlane(wave) * 16 * NC;
+    const int len = kv4_len(a.c, k.s), c0 = k.c0 + wave * 16 * NC;
     if (c0 >= k.n) return;
-    Kv4Query<D> x[NC];
+    Kv4Query<D, sizeof(T) == 4> x[NC];
     int lim[NC], most = 0, least = 1 << 30;
     Kv4Column col[NC];
 #pragma unroll
@@ -680,25 +725,24 @@ __global__ __launch_bounds__(256, 1) void kv4_attend_many_kernel(const Kv4Attn a
         lim[n] = col[n].lim;
         most = max(most, lanes_max(lim[n])); least = min(least, lanes_min(live ? lim[n] : 1 << 30));
         const T *row = (const T *)a.q + (size_t)col[n].row * a.q_stride + (size_t)col[n].head * D;
-        x[n].load(row, live, ((uintptr_t)a.q | (uintptr_t)a.q_stride * sizeof(T)) % (8 * sizeof(T)) == 0, a.scale, q);
+        x[n].load(row, live, kv4_aligned<T>(a.q, a.q_stride, 8), a.scale, q);
     }
     const int t0 = chunk * a.chunk, t1 = min(most, t0 + a.chunk);
     if (t0 >= t1 && chunk > 0) return;
     Kv4State<D, NC> state;
     state.clear();
-    kv4_run<D, NC>(a.c, k.s, h, state, x, lim, least, t0, t1, 32, lane);
+    kv4_run(a.c, k.s, h, state, x, lim, least, t0, t1, 32, lane);
     state.finish();
-    const bool aligned = ((uintptr_t)a.out | (uintptr_t)a.out_stride * sizeof(T)) % (4 * sizeof(T)) == 0;
+    const bool aligned = kv4_aligned<T>(a.out, a.out_stride, 4);
 #pragma unroll
     for (int n = 0; n < NC; n++) {
         if (c0 + 16 * n + (lane & 15) >= k.n) continue;
         const float l = state.l[n];
         if (a.n_chunks > 1) {
-            float *p = a.part + (((size_t)chunk * a.n_rows + col[n].row) * a.heads + col[n].head) * (D + 2);
+            const size_t at = ((size_t)col[n].row * a.heads + col[n].head) * a.n_chunks + chunk;
 #pragma unroll
-            for (int j = 0; j < DT; j++)
-                for (int i = 0; i < 4; i++) p[16 * j + 4 * q + i] = state.o[n][j][i];
-            if (q == 0) { p[D] = state.m[n]; p[D + 1] = l; }
+            for (int j = 0; j < DT; j++) *(f32x4_t *)(a.part + at * D + 16 * j + 4 * q) = state.o[n][j];
+            if (q == 0) a.part_ml[at] = float2{state.m[n], l};
         } else {
             T *out = (T *)a.out + (size_t)col[n].row * a.out_stride + (size_t)col[n].head * D;
 #pragma unroll
@@ -707,39 +751,47 @@ __global__ __launch_bounds__(256, 1) void kv4_attend_many_kernel(const Kv4Attn a
                 for (int i = 0; i < 4; i++) o[i] = l == 0.f ? 0.f : state.o[n][j][i] / l;
                 kv4_store4(out + 16 * j + 4 * q, aligned, o);
             }
-            if (q == 0) a.lse[(size_t)col[n].row * a.heads + col[n].head] = l == 0.f ? -INFINITY : state.m[n] - 14.f + __builtin_amdgcn_logf(l);
+            if (q == 0) a.lse[(size_t)col[n].row * a.heads + col[n].head] = l == 0.f ? -INFINITY : state.m[n] - KV4_SHIFT + __builtin_amdgcn_logf(l);
         }
     }
 }
 
-// Joins the chunks of a row and head: a wave each.
+// Joins the chunks of a row and head, a workgroup each: wave w takes chunks w, w + 4, .., lane j of it the reference and sum of the j-th.
+// Chunks behind the last token that any column of the row's block sees were not written; they end no earlier than the row's own.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_join_kernel(const Kv4Attn a)
 {
-    const int lane = threadIdx.x & 63;
-    const size_t item = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (item >= (size_t)a.n_rows * a.heads) return;
-    const int r = (int)(item / a.heads), hq = (int)(item % a.heads);
+    __shared__ float os[4][D], ms[4], ls[4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = blockIdx.x / a.heads, hq = blockIdx.x % a.heads;
     const Kv4Row row = kv4_row(a.c, a.row_start, r);
     if (row.s < 0) return;
-    // Chunks behind the last token that any column of the row's block sees were not written.  They end no earlier than the row's own.
-    const int lim = max(0, min(row.pos + 1, a.max_len)), n = max(1, (lim + a.chunk - 1) / a.chunk);
-    const float *p = a.part + ((size_t)r * a.heads + hq) * (D + 2);
-    const size_t step = (size_t)a.n_rows * a.heads * (D + 2);
-    float m = -INFINITY;
-    for (int i = 0; i < n; i++) m = fmaxf(m, p[i * step + D]);
-    const float ref = m == -INFINITY ? 0.f : m;
-    float l = 0.f, o[D / 64] = {};
-    for (int i = 0; i < n; i++) {
-        const float f = __builtin_amdgcn_exp2f(p[i * step + D] - ref);
-        l = fmaf(f, p[i * step + D + 1], l);
+    const int lim = max(0, min(row.pos + 1, a.max_len)), n = max(1, (lim + a.chunk - 1) / a.chunk), mine = (n - wave + 3) / 4;
+    const float2 *ml = a.part_ml + (size_t)blockIdx.x * a.n_chunks;
+    const float *p = a.part + ((size_t)blockIdx.x * a.n_chunks + wave) * D + lane;
+    const float2 c = lane < mine ? ml[wave + 4 * lane] : float2{-INFINITY, 0.f};
+    float m = wave_max(c.x);
+    if (lane == 0) ms[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
+    const float f = __builtin_amdgcn_exp2f(c.x - (m == -INFINITY ? 0.f : m));
+    const float l = wave_sum(f * c.y);
+    float o[D / 64] = {};
+#pragma unroll 8
+    for (int j = 0; j < mine; j++) {
+        const float fj = lane_value(f, j);
 #pragma unroll
-        for (int e = 0; e < D / 64; e++) o[e] = fmaf(f, p[i * step + lane + 64 * e], o[e]);
+        for (int e = 0; e < D / 64; e++) o[e] = fmaf(fj, p[(size_t)j * 4 * D + 64 * e], o[e]);
     }
-    T *out = (T *)a.out + (size_t)r * a.out_stride + (size_t)hq * D;
+    if (lane == 0) ls[wave] = l;
 #pragma unroll
-    for (int e = 0; e < D / 64; e++) out[lane + 64 * e] = (T)(l == 0.f ? 0.f : o[e] / l);
-    if (lane == 0) a.lse[(size_t)r * a.heads + hq] = l == 0.f ? -INFINITY : m - 14.f + __builtin_amdgcn_logf(l);
+    for (int e = 0; e < D / 64; e++) os[wave][lane + 64 * e] = o[e];
+    __syncthreads();
+    const float total = (ls[0] + ls[1]) + (ls[2] + ls[3]);
+    if (threadIdx.x < D) {
+        const float v = (os[0][threadIdx.x] + os[1][threadIdx.x]) + (os[2][threadIdx.x] + os[3][threadIdx.x]);
+        ((T *)a.out)[(size_t)r * a.out_stride + (size_t)hq * D + threadIdx.x] = (T)(total == 0.f ? 0.f : v / total);
+    }
+    if (threadIdx.x == 0) a.lse[blockIdx.x] = total == 0.f ? -INFINITY : m - KV4_SHIFT + __builtin_amdgcn_logf(total);
 }
 
 // w_out[s][h][t] = w_in + the probabilities of token t, summed over the rows and the query heads of head h.  A wave takes 32 tokens and goes over
@@ -762,14 +814,14 @@ __global__ __launch_bounds__(256, 2) void kv4_weights_kernel(const Kv4Attn a)
 #pragma unroll
     for (int i = 0; i < 2; i++) { keys[i].load(st.blk[i], P, st.t[i], lane); keys[i].widen(kk[i]); }
     float sum[8] = {};
-    const bool aligned = ((uintptr_t)a.q | (uintptr_t)a.q_stride * sizeof(T)) % (8 * sizeof(T)) == 0;
+    const bool aligned = kv4_aligned<T>(a.q, a.q_stride, 8);
     // columns in front of the first that sees token t0 see none of these
     int first = t0 - (len - k.end + k.r0);
     first = first > 0 && t0 < n ? min(first, k.n) * a.group : 0;
     for (int c0 = min(first, k.n) & ~15; c0 < k.n; c0 += 16) {
         const Kv4Column col = kv4_column(a, k, h, c0 + (lane & 15), len);
         const bool live = c0 + (lane & 15) < k.n;
-        Kv4Query<D> x;
+        Kv4Query<D, sizeof(T) == 4> x;
         x.load((const T *)a.q + (size_t)col.row * a.q_stride + (size_t)col.head * D, live, aligned, a.scale, q);
         const float lse = live ? a.lse[(size_t)col.row * a.heads + col.head] : 0.f;
 #pragma unroll
@@ -782,8 +834,7 @@ __global__ __launch_bounds__(256, 2) void kv4_weights_kernel(const Kv4Attn a)
     }
     // over the 16 columns of a tile
 #pragma unroll
-    for (int j = 0; j < 8; j++)
-        for (int o = 1; o < 16; o <<= 1) sum[j] += __shfl_xor(sum[j], o);
+    for (int j = 0; j < 8; j++) sum[j] = row_sum(sum[j]);
     const size_t at = ((size_t)s * a.c.H + h) * ((size_t)a.c.max_pages << a.c.logT);
 #pragma unroll
     for (int j = 0; j < 8; j++) {
@@ -811,14 +862,41 @@ struct Kv4Evict {
     int *kept;
 };
 
-// Which tokens of a sequence and head stay: radix selection of the need-th largest weight (four digits of 8 bits), then the tokens
-// in order with their ranks.  One workgroup per sequence and head.
+// Which tokens of a sequence and head stay: radix selection of the need-th largest weight (digits of 11, 11 and 10 bits), then the tokens
+// in order with their ranks.  One workgroup per sequence and head.  A thread takes consecutive tokens, up to 32 of a segment of 32768, so
+// that one scan over the workgroup ranks a whole segment; the weights come from the L2 again in every pass.  Weights share few exponents,
+// so the histogram is held eight times over (lane % 8) against conflicts.  4096 of 32 heads: 9 us; with digits of 8 bits, one histogram
+// and a serial search of it 36.
+constexpr int KV4_SEG = 32, KV4_COPIES = 8;
+__device__ __forceinline__ int block_scan(int v, int *tmp, int &total)     // exclusive, 1024 threads; tmp [16]
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int x = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(x, o);
+        if (lane >= o) x += u;
+    }
+    __syncthreads();                            // (tmp of an earlier scan has been read)
+    if (lane == 63) tmp[wave] = x;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+        const int t = tmp[i];
+        before += i < wave ? t : 0;
+        total += t;
+    }
+    return before + x - v;
+}
+
 __global__ __launch_bounds__(1024) void kv4_select_kernel(const Kv4Evict a)
 {
-    __shared__ int hist[256], scan[16], digit, left;
-    const int s = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ int hist[2048 * KV4_COPIES], tmp[16], found[2];
+    const int s = blockIdx.y, h = blockIdx.x, tid = threadIdx.x;
     const size_t in_cap = (size_t)a.src.max_pages << a.src.logT, out_cap = (size_t)a.dst.max_pages << a.dst.logT;
-    const float *w = a.w_in + ((size_t)s * a.src.H + h) * in_cap;
+    const float *w = a.w_in + ((size_t)s * a.src.H + h) * in_cap;       // (in_cap is a multiple of 16, so every row is 16-byte aligned if the first is)
     float *wo = a.w_out + ((size_t)s * a.src.H + h) * out_cap;
     int *kept = a.kept + ((size_t)s * a.src.H + h) * a.keep;
     const int n = kv4_len(a.src, s), m = min(n, a.keep);
@@ -829,79 +907,146 @@ __global__ __launch_bounds__(1024) void kv4_select_kernel(const Kv4Evict a)
         return;
     }
     const int lo = a.first, hi = n - a.recent, need = a.keep - a.first - a.recent;
+    // tokens per thread and segment: a multiple of 4
+    const int per = min(KV4_SEG, (n + 4095) / 4096 * 4), seg = per * 1024;
+    const bool aligned = ((uintptr_t)a.w_in & 15) == 0;
+    auto load4 = [&](int t, float (&x)[4]) {    // tokens t..t + 3, t a multiple of 4 below n (a row's memory goes on to a multiple of 16)
+        if (aligned) {
+            const float4 v = *(const float4 *)(w + t);
+            x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; e++) x[e] = w[t + e];
+        }
+    };
     uint32_t prefix = 0;
     int want = need;                            // of the candidates whose leading digits are prefix's
-    for (int shift = 24; shift >= 0 && need; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
+#pragma unroll
+    for (int pass = 0; pass < 3; pass++) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass < 2 ? 11 : 10;
+        if (!need) break;
+        for (int i = tid; i < 2048 * KV4_COPIES; i += 1024) hist[i] = 0;
         __syncthreads();
-        for (int i = lo + tid; i < hi; i += 1024) {
-            const uint32_t k = kv4_key(w[i]);
-            if (shift == 24 || k >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&hist[k >> shift & 255], 1);
+        for (int s0 = 0; s0 < n; s0 += seg) {
+#pragma unroll
+            for (int i = 0; i < KV4_SEG / 4; i++) {
+                const int t = s0 + i * 4096 + tid * 4;          // (here the order does not matter: neighbouring lanes read neighbouring tokens)
+                if (i * 4 >= per || t >= n) continue;
+                float x[4];
+                load4(t, x);
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const uint32_t k = kv4_key(x[e]);
+                    if (t + e >= lo && t + e < hi && (pass == 0 || k >> (shift + bits) == prefix >> (shift + bits)))
+                        atomicAdd(&hist[(k >> shift & ((1u << bits) - 1)) * KV4_COPIES + (tid & (KV4_COPIES - 1))], 1);
+                }
+            }
         }
         __syncthreads();
-        if (tid == 0) {
-            int c = 0, d = 255;
-            while (d > 0 && c + hist[d] < want) c += hist[d--];
-            digit = d; left = want - c;
+        // thread i looks at digits 2047 - 2 i and 2046 - 2 i: how many candidates lie above them
+        int c[2];
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+            c[e] = 0;
+#pragma unroll
+            for (int j = 0; j < KV4_COPIES; j++) c[e] += hist[(2047 - 2 * tid - e) * KV4_COPIES + j];
+        }
+        int total, above = block_scan(c[0] + c[1], tmp, total);
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+            if (above < want && above + c[e] >= want) { found[0] = 2047 - 2 * tid - e; found[1] = want - above; }
+            above += c[e];
         }
         __syncthreads();
-        prefix |= (uint32_t)digit << shift;
-        want = left;
+        prefix |= (uint32_t)found[0] << shift;
+        want = found[1];
         __syncthreads();
     }
     // tokens above the threshold, and the first `want` that equal it
     int above = 0, equal = 0;
-    for (int t0 = 0; t0 < n; t0 += 1024) {
-        const int t = t0 + tid;
-        int f = 0;                              // 1: stays, 0x10000: equals the threshold
-        if (t < n) {
-            if (t < lo || t >= hi) f = 1;
-            else if (need) {
-                const uint32_t k = kv4_key(w[t]);
-                f = k > prefix ? 1 : k == prefix ? 0x10000 : 0;
+    for (int s0 = 0; s0 < n; s0 += seg) {
+        const int t0 = s0 + tid * per;
+        uint32_t up = 0, eq = 0;
+#pragma unroll
+        for (int i = 0; i < KV4_SEG / 4; i++) {
+            const int t = t0 + 4 * i;
+            if (i * 4 >= per || t >= n) continue;
+            float x[4];
+            load4(t, x);
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const uint32_t k = kv4_key(x[e]);
+                const bool in = t + e < n, forced = in && (t + e < lo || t + e >= hi), cand = in && !forced && need;
+                up |= (uint32_t)(forced || (cand && k > prefix)) << (4 * i + e);
+                eq |= (uint32_t)(cand && k == prefix) << (4 * i + e);
             }
         }
-        int v = f;
-        for (int o = 1; o < 64; o <<= 1) {
-            const int u = __shfl_up(v, o);
-            if (lane >= o) v += u;
+        int total_up, total_eq;
+        const int before_up = block_scan(__popc(up), tmp, total_up), before_eq = block_scan(__popc(eq), tmp, total_eq);
+        int pos = above + before_up + min(equal + before_eq, want), ties = equal + before_eq;
+        for (uint32_t any = up | eq; any; any &= any - 1) {
+            const int i = __builtin_ctz(any);
+            if (eq >> i & 1) {
+                if (ties >= want) continue;
+                ties++;
+            }
+            kept[pos] = t0 + i; wo[pos] = w[t0 + i];
+            pos++;
         }
-        if (lane == 63) scan[wave] = v;
-        __syncthreads();
-        int before = 0, total = 0;
-        for (int i = 0; i < 16; i++) {
-            if (i < wave) before += scan[i];
-            total += scan[i];
-        }
-        __syncthreads();
-        const int ex = before + v - f, e = equal + (ex >> 16), pos = above + (ex & 0xffff) + min(e, want);
-        if (f == 1 || (f && e < want)) { kept[pos] = t; wo[pos] = w[t]; }
-        above += total & 0xffff; equal += total >> 16;
+        above += total_up; equal += total_eq;
     }
 }
 
-// The kept tokens' numbers, moved together.  Four tokens of the new page per 16 lanes.
+// The kept tokens' numbers, moved together.  Four tokens of the new page per 16 lanes: lane l carries piece l % 4 of the keys of token l / 4, the
+// values' halfwords r = l of all four, and one number of each of the four tables of scales.
 template <int D>
 __global__ __launch_bounds__(256) void kv4_move_kernel(const Kv4Evict a)
 {
     typedef Kv4<D> L;
+    constexpr int G = L::G, VH = L::VH, KW = D / 32;        // words of a lane's piece of a token's keys
     const int s = blockIdx.z, h = blockIdx.y, li = threadIdx.x & 15, quad = blockIdx.x * 16 + (threadIdx.x >> 4);
     const int P = 1 << a.src.logT, Q = 1 << a.dst.logT, n = kv4_len(a.src, s), m = min(n, a.keep);
     if (quad * 4 >= m) return;
-    char *dst = (quad * 4 >> a.dst.logT) < a.dst.max_pages ? kv4_block<D>(a.dst, s, h, quad * 4) : nullptr;
+    char *dst = kv4_block<D>(a.dst, s, h, quad * 4);        // (quad * 4 < n_keep, which the page table reaches)
     if (!dst) return;
     const int *kept = a.kept + ((size_t)s * a.src.H + h) * a.keep + quad * 4;
-    for (int i = 0; i < 4 && quad * 4 + i < m; i++) {
-        const int from = kept[i], t = from & (P - 1), u = (quad * 4 + i) & (Q - 1);
-        const char *src = kv4_block<D>(a.src, s, h, from);
-        for (int w = li; w < D / 8; w += 16) *(uint32_t *)(dst + u * (D / 2) + 4 * w) = src ? *(const uint32_t *)(src + t * (D / 2) + 4 * w) : 0;
-        for (int k = 0; k < L::VH; k++)
-            *(uint16_t *)(dst + L::v_half(Q, u, li, k)) = src ? *(const uint16_t *)(src + L::v_half(P, t, li, k)) : 0;
-        if (li < L::G) {
-            *(uint16_t *)(dst + L::ks(Q, u, li)) = src ? *(const uint16_t *)(src + L::ks(P, t, li)) : 0;
-            *(uint16_t *)(dst + L::km(Q, u, li)) = src ? *(const uint16_t *)(src + L::km(P, t, li)) : 0;
-            *(uint16_t *)(dst + L::vs(Q, u, li)) = src ? *(const uint16_t *)(src + L::vs(P, t, li)) : 0;
-            *(uint16_t *)(dst + L::vm(Q, u, li)) = src ? *(const uint16_t *)(src + L::vm(P, t, li)) : 0;
+    const int u = quad * 4 & (Q - 1), last = m - quad * 4;  // tokens of the quad that there are, if fewer than 4
+    const char *src[4];
+    int t[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const int from = i < last ? kept[i] : 0;
+        t[i] = from & (P - 1);
+        src[i] = i < last ? kv4_block<D>(a.src, s, h, from) : nullptr;
+    }
+    // the lane's own token of the four
+    const int mine = li >> 2, piece = li & 3;
+    const char *ms = mine == 0 ? src[0] : mine == 1 ? src[1] : mine == 2 ? src[2] : src[3];
+    const int mt = mine == 0 ? t[0] : mine == 1 ? t[1] : mine == 2 ? t[2] : t[3];
+    uint32_t kw[KW] = {};
+    uint16_t vw[VH][4] = {}, ks = 0, km = 0, vs = 0, vm = 0;
+    if (ms) {
+        __builtin_memcpy(kw, __builtin_assume_aligned(ms + mt * (D / 2) + piece * 4 * KW, 4 * KW), 4 * KW);
+        if (piece < G) {
+            ks = *(const uint16_t *)(ms + L::ks(P, mt, piece)); km = *(const uint16_t *)(ms + L::km(P, mt, piece));
+            vs = *(const uint16_t *)(ms + L::vs(P, mt, piece)); vm = *(const uint16_t *)(ms + L::vm(P, mt, piece));
         }
     }
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        if (src[i])
+#pragma unroll
+            for (int k = 0; k < VH; k++) vw[k][i] = *(const uint16_t *)(src[i] + L::v_half(P, t[i], li, k));
+    if (mine < last) {
+        __builtin_memcpy(__builtin_assume_aligned(dst + (u + mine) * (D / 2) + piece * 4 * KW, 4 * KW), kw, 4 * KW);
+        if (piece < G) {
+            *(uint16_t *)(dst + L::ks(Q, u + mine, piece)) = ks; *(uint16_t *)(dst + L::km(Q, u + mine, piece)) = km;
+            *(uint16_t *)(dst + L::vs(Q, u + mine, piece)) = vs; *(uint16_t *)(dst + L::vm(Q, u + mine, piece)) = vm;
+        }
+    }
+    if (last >= 4) __builtin_memcpy(__builtin_assume_aligned(dst + L::v_half(Q, u, li, 0), 8 * VH), vw, 8 * VH);
+    else
+        for (int i = 0; i < last; i++)
+#pragma unroll
+            for (int k = 0; k < VH; k++) *(uint16_t *)(dst + L::v_half(Q, u + i, li, k)) = vw[k][i];
 }
