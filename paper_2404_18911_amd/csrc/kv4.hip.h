@@ -269,6 +269,7 @@ struct Kv4Attn {
 };
 
 constexpr float KV4_SHIFT = 28.f;
+constexpr int KV4_RING = 3;
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 union Kv4Op { uint32_t w[4]; f16x8_t v; };
 
@@ -389,18 +390,64 @@ template <int D, bool LO> struct Kv4Query {
     }
 };
 
+// A step's numbers in LDS, brought there without passing registers (lds_load16: 16 bytes a lane, lane after lane, from any addresses):
+// keys of both tiles as their readers want them, values likewise, then for each tile its parts of the four tables.
+template <int D> struct Kv4Stage {
+    static constexpr int G = D / 32, BYTES = D == 128 ? 5120 : 3072, LOADS = D == 128 ? 5 : 3;
+    static __device__ __forceinline__ int k_read(int i, int lane)
+    {
+        return D == 128 ? i * 1024 + lane * 16 : i * 512 + ((lane & 15) + (lane >> 5) * 16) * 16 + (lane >> 4 & 1) * 8;
+    }
+    static __device__ __forceinline__ int v_read(int i, int lane) { return D == 128 ? 2048 + i * 1024 + lane * 16 : 1024 + i * 512 + lane * 8; }
+    static __device__ __forceinline__ int table(int i, int n) { return D == 128 ? 4096 + i * 512 + n * 128 : 2048 + i * 256 + n * 64; }
+    // load n of the LOADS of a step: blocks b0, b1 of the tiles and their first tokens t0, t1 in the page
+    static __device__ __forceinline__ void load(int n, const char *b0, int t0, const char *b1, int t1, int P, uint32_t lds, int lane)
+    {
+        if (D == 128) {
+            const char *b = n & 1 ? b1 : b0;
+            const int t = n & 1 ? t1 : t0;
+            if (n < 2) lds_load16(b + t * 64, (lane & 15) * 64 + (lane >> 4) * 16, lds + n * 1024);
+            else if (n < 4) lds_load16(b + P * 64 + t * 64, lane * 16, lds + n * 1024);
+            else {
+                const char *x = lane < 32 ? b0 + t0 * 8 : b1 + t1 * 8;
+                lds_load16(x + P * D + (lane >> 3 & 3) * 8 * P + (lane & 7) * 16, lds + 4096);
+            }
+        } else {
+            const int l = lane & 31;
+            if (n == 0) lds_load16((lane < 32 ? b0 + t0 * 32 : b1 + t1 * 32) + (l & 15) * 32 + (l >> 4) * 16, lds);
+            else if (n == 1) lds_load16((lane < 32 ? b0 + t0 * 32 : b1 + t1 * 32) + P * 32 + l * 16, lds + 1024);
+            else {              // 32 lanes' worth; the others repeat them behind
+                const char *x = (l < 16 ? b0 + t0 * 4 : b1 + t1 * 4);
+                lds_load16(x + P * D + (l >> 2 & 3) * 4 * P + (l & 3) * 16, lds + 2048);
+            }
+        }
+    }
+};
+// until at most n loads are under way
+template <int N> __device__ __forceinline__ void loads_left() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+// what was read from LDS has arrived: the place may be written again
+__device__ __forceinline__ void lds_reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // The numbers of one tile of 16 tokens as they lie in the page.
 template <int D> struct Kv4Keys {
     static constexpr int G = D / 32;
     uint32_t w[G], s[2 * G], m[G / 2];      // lane's token: words; tokens 4 q + 0..3: scales; lane's token: minima
 
-    // tile of tokens t.. of the page (t a multiple of 16); block and t are the wave's, the lane's part comes as 32-bit offsets
-    __device__ __forceinline__ void load(const char *blk, int P, int t, int lane)
+    // tile of tokens t.. of a page
+    __device__ __forceinline__ void load_page(const char *blk, int P, int t, int lane)
     {
         const uint32_t q = lane >> 4, tok = lane & 15;
         __builtin_memcpy(w, __builtin_assume_aligned(blk + Kv4<D>::k_word(P, t, 0, 0) + (tok * (D / 2) + q * 4 * G), 4 * G), 4 * G);
         __builtin_memcpy(s, __builtin_assume_aligned(blk + Kv4<D>::ks(P, t, 0) + q * 8 * G, 16), 8 * G);
         __builtin_memcpy(m, __builtin_assume_aligned(blk + Kv4<D>::km(P, t, 0) + tok * 2 * G, 2 * G), 2 * G);
+    }
+    // tile i of a step in LDS (Kv4Stage)
+    __device__ __forceinline__ void load(const char *stage, int i, int lane)
+    {
+        const int q = lane >> 4, tok = lane & 15;
+        __builtin_memcpy(w, __builtin_assume_aligned(stage + Kv4Stage<D>::k_read(i, lane), 4 * G), 4 * G);
+        __builtin_memcpy(s, __builtin_assume_aligned(stage + Kv4Stage<D>::table(i, 0) + q * 8 * G, 16), 8 * G);
+        __builtin_memcpy(m, __builtin_assume_aligned(stage + Kv4Stage<D>::table(i, 1) + tok * 2 * G, 2 * G), 2 * G);
     }
     // the levels as the other side of the score instructions
     __device__ __forceinline__ void widen(f16x8_t (&k)[G]) const
@@ -430,32 +477,26 @@ template <int D> struct Kv4Keys {
         return z;
     }
 };
-template <int D> struct Kv4Values {
-    static constexpr int G = D / 32, VH = D / 64;
-    uint32_t w[2 * VH], s[2 * G], m[2 * G]; // tokens 4 q + 0..3: words of lane % 16, scales, minima
-
-    __device__ __forceinline__ void load(const char *blk, int P, int t, int lane)
-    {
-        const uint32_t q = lane >> 4;
-        __builtin_memcpy(w, __builtin_assume_aligned(blk + Kv4<D>::v_half(P, t, 0, 0) + (uint32_t)lane * 8 * VH, 8 * VH), 8 * VH);
-        __builtin_memcpy(s, __builtin_assume_aligned(blk + Kv4<D>::vs(P, t, 0) + q * 8 * G, 16), 8 * G);
-        __builtin_memcpy(m, __builtin_assume_aligned(blk + Kv4<D>::vm(P, t, 0) + q * 8 * G, 16), 8 * G);
-    }
-    // e of the tokens' largest scales, s < 2^(e - 14) (of garbage: 0..31).  Scales are not negative, so halves compare as whole numbers.
-    __device__ __forceinline__ void exponents(float (&e)[4]) const
-    {
-        typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+// e of the tokens' largest value scales, s < 2^(e - 14) (of garbage: 0..31).  Scales are not negative, so halves compare as whole numbers.
+template <int G> __device__ __forceinline__ void kv4_exponents(const uint32_t (&s)[2 * G], float (&e)[4])
+{
+    typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
 #pragma unroll
-        for (int a = 0; a < 2; a++) {
-            u16x2_t mx = __builtin_bit_cast(u16x2_t, s[a]);
+    for (int a = 0; a < 2; a++) {
+        u16x2_t mx = __builtin_bit_cast(u16x2_t, s[a]);
 #pragma unroll
-            for (int g = 1; g < G; g++) mx = __builtin_elementwise_max(mx, __builtin_bit_cast(u16x2_t, s[2 * g + a]));
-            const uint32_t w = __builtin_bit_cast(uint32_t, mx);
-            e[2 * a] = (float)(w >> 10 & 31);
-            e[2 * a + 1] = (float)(w >> 26 & 31);
-        }
+        for (int g = 1; g < G; g++) mx = __builtin_elementwise_max(mx, __builtin_bit_cast(u16x2_t, s[2 * g + a]));
+        const uint32_t w = __builtin_bit_cast(uint32_t, mx);
+        e[2 * a] = (float)(w >> 10 & 31);
+        e[2 * a + 1] = (float)(w >> 26 & 31);
     }
-};
+}
+template <int N> __device__ __forceinline__ void lds_read(uint32_t (&x)[N], const char *p)
+{
+    __builtin_memcpy(x, __builtin_assume_aligned(p, N >= 4 ? 16 : 4 * N), 4 * N);
+}
+// what comes behind is not begun before what stands in front: keeps the numbers of a later part of a step out of the registers
+#define KV4_PART __builtin_amdgcn_sched_barrier(0)
 
 // The step's two tiles: where they lie (null: no page, none of its tokens is seen).
 struct Kv4Step { const char *blk[2]; int t[2]; bool here[2]; };
@@ -463,12 +504,13 @@ template <int D> __device__ __forceinline__ Kv4Step kv4_step(const Kv4View &c, i
 {
     Kv4Step st;
     const int P = 1 << c.logT;
+    // (constant memory while the kernel runs: scalar loads, which do not queue behind the loads that fill the LDS)
+    const __attribute__((address_space(4))) int *table = (const __attribute__((address_space(4))) int *)(c.table + (size_t)s * c.max_pages);
 #pragma unroll
     for (int i = 0; i < 2; i++) {
         const int t = t0 + 16 * i;
         int page = -1;
-        if (t < limit) page = c.table[(size_t)s * c.max_pages + (t >> c.logT)];
-        page = __builtin_amdgcn_readfirstlane(page);
+        if (t < limit) page = table[t >> c.logT];
         st.here[i] = page >= 0 && page < c.n_pages;
         st.t[i] = st.here[i] ? t & (P - 1) : 0;                 // (a tile that is not there is read as page 0 and masked)
         st.blk[i] = c.pool + (size_t)(st.here[i] ? page : 0) * c.page_stride + (size_t)h * Kv4<D>::block(P);
@@ -492,37 +534,47 @@ template <int D, int NC> struct Kv4State {
             m[n] = -INFINITY; l[n] = 0.f;
         }
     }
-    // One step of 32 tokens from t0 on.  MASK: lim[n] is the number of tokens that the lane's column sees.
+    // One step of 32 tokens from t0 on, its numbers in LDS.  MASK: lim[n] is the number of tokens that the lane's column sees, here: the tiles that
+    // have a page.  Written so that few of the step's numbers are in registers at a time.
     template <bool MASK, bool LO>
-    __device__ __forceinline__ void step(const Kv4Query<D, LO> (&x)[NC], const Kv4Keys<D> (&k)[2], const Kv4Values<D> (&v)[2], const int (&lim)[NC],
-                                         const Kv4Step &st, int t0, int q)
+    __device__ __forceinline__ void step(const Kv4Query<D, LO> (&x)[NC], const char *stage, const int (&lim)[NC], int here, int t0, int lane)
     {
 #pragma clang fp contract(off)                      // (both instances of MASK round alike: a row's bits do not depend on which one it went through)
+        typedef Kv4Stage<D> S;
+        const int q = lane >> 4;
         float z[NC][8], e[8];
 #pragma unroll
         for (int i = 0; i < 2; i++) {
+            Kv4Keys<D> k;
+            k.load(stage, i, lane);
             f16x8_t kk[G];
-            k[i].widen(kk);
+            k.widen(kk);
 #pragma unroll
             for (int n = 0; n < NC; n++) {
-                const f32x4_t zz = k[i].scores(kk, x[n]);
+                const f32x4_t zz = k.scores(kk, x[n]);
 #pragma unroll
                 for (int j = 0; j < 4; j++) z[n][4 * i + j] = zz[j] * x[n].f;
             }
+        }
+        KV4_PART;
+        uint32_t vs[2][2 * G];
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
             float ee[4];
-            v[i].exponents(ee);
+            lds_read(vs[i], stage + S::table(i, 2) + q * 8 * G);
+            kv4_exponents<G>(vs[i], ee);
 #pragma unroll
             for (int j = 0; j < 4; j++) e[4 * i + j] = ee[j];
         }
-        uint32_t ph[NC][G][4], pl[NC][G][4];
+        bool see[NC][8];
+        float p[NC][8];
 #pragma unroll
         for (int n = 0; n < NC; n++) {
-            bool see[8];
             float mx = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 8; j++) {
-                see[j] = !MASK || (st.here[j >> 2] && t0 + 16 * (j >> 2) + 4 * q + (j & 3) < lim[n]);
-                if (!see[j]) z[n][j] = -INFINITY;
+                see[n][j] = !MASK || ((here >> (j >> 2) & 1) && t0 + 16 * (j >> 2) + 4 * q + (j & 3) < lim[n]);
+                if (!see[n][j]) z[n][j] = -INFINITY;
                 mx = fmaxf(mx, z[n][j] + e[j]);
             }
             mx = quads_max(mx);
@@ -536,43 +588,50 @@ template <int D, int NC> struct Kv4State {
                 m[n] = m_new;
             }
             const float ref = (m[n] == -INFINITY ? 0.f : m[n]) - KV4_SHIFT;
-            float p[8];
 #pragma unroll
             for (int j = 0; j < 8; j++) {
-                p[j] = __builtin_amdgcn_exp2f(z[n][j] - ref);
-                l[n] += p[j];
+                p[n][j] = __builtin_amdgcn_exp2f(z[n][j] - ref);
+                l[n] += p[n][j];
             }
-#pragma unroll
-            for (int g = 0; g < G; g++)
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    const uint32_t sw = v[j >> 2].s[2 * g + (j >> 1 & 1)], mw = v[j >> 2].m[2 * g + (j >> 1 & 1)];
-                    const float x0 = see[j] ? fmaf(p[j], half_of(sw, 0), 0.f) : 0.f, x1 = see[j + 1] ? fmaf(p[j + 1], half_of(sw, 1), 0.f) : 0.f;
-                    kv4_split(x0, x1, ph[n][g][j >> 1], pl[n][g][j >> 1]);
-                    if (see[j]) om[n][g] = fmaf(p[j], half_of(mw, 0), om[n][g]);
-                    if (see[j + 1]) om[n][g] = fmaf(p[j + 1], half_of(mw, 1), om[n][g]);
-                }
         }
+        KV4_PART;
         constexpr int VH = D / 64;
+        uint32_t vw[2][2 * VH];
+#pragma unroll
+        for (int i = 0; i < 2; i++) lds_read(vw[i], stage + S::v_read(i, lane));
 #pragma unroll
         for (int h = 0; h < VH; h++) {
-            uint32_t u[4][4];
+            uint32_t u[4][4];                       // nibbles i of the halfwords
 #pragma unroll
-            for (int a = 0; a < 4; a++) kv4_widen(v[a >> 1].w[2 * h + (a & 1)], u[a]);
+            for (int a = 0; a < 4; a++) kv4_widen(vw[a >> 1][2 * h + (a & 1)], u[a]);
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                // nibble i of a word's halves; kv4_widen numbers the nibbles of a half 0, 1, 2, 3
-                Kv4Op a;
+            for (int g = 2 * h; g < 2 * h + 2; g++) {
+                uint32_t vm[2][2];
 #pragma unroll
-                for (int w = 0; w < 4; w++) a.w[w] = u[w][i];
-                const int j = 4 * h + i;
+                for (int i = 0; i < 2; i++) lds_read(vm[i], stage + S::table(i, 3) + (q * G + g) * 8);
+                Kv4Op hi[NC], lo[NC];
 #pragma unroll
-                for (int n = 0; n < NC; n++) {
-                    Kv4Op hi, lo;
+                for (int n = 0; n < NC; n++)
 #pragma unroll
-                    for (int w = 0; w < 4; w++) { hi.w[w] = ph[n][j >> 1][w]; lo.w[w] = pl[n][j >> 1][w]; }
-                    o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, hi.v, o[n][j], 0, 0, 0);
-                    o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, lo.v, o[n][j], 0, 0, 0);
+                    for (int j = 0; j < 8; j += 2) {
+                        const uint32_t sw = vs[j >> 2][2 * g + (j >> 1 & 1)], mw = vm[j >> 2][j >> 1 & 1];
+                        const float x0 = see[n][j] ? fmaf(p[n][j], half_of(sw, 0), 0.f) : 0.f, x1 = see[n][j + 1] ? fmaf(p[n][j + 1], half_of(sw, 1), 0.f) : 0.f;
+                        kv4_split(x0, x1, hi[n].w[j >> 1], lo[n].w[j >> 1]);
+                        const float y0 = fmaf(p[n][j], half_of(mw, 0), om[n][g]);
+                        om[n][g] = see[n][j] ? y0 : om[n][g];
+                        const float y1 = fmaf(p[n][j + 1], half_of(mw, 1), om[n][g]);
+                        om[n][g] = see[n][j + 1] ? y1 : om[n][g];
+                    }
+#pragma unroll
+                for (int j = 2 * g; j < 2 * g + 2; j++) {
+                    Kv4Op a;
+#pragma unroll
+                    for (int w = 0; w < 4; w++) a.w[w] = u[w][j & 3];
+#pragma unroll
+                    for (int n = 0; n < NC; n++) {
+                        o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, hi[n].v, o[n][j], 0, 0, 0);
+                        o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, lo[n].v, o[n][j], 0, 0, 0);
+                    }
                 }
             }
         }
@@ -593,24 +652,48 @@ template <int D, int NC> struct Kv4State {
     }
 };
 
-// steps t0, t0 + stride, .. below t1 of the columns x
-template <int D, int NC, bool LO>
-__device__ __forceinline__ void kv4_run(const Kv4View &c, int s, int h, Kv4State<D, NC> &state, const Kv4Query<D, LO> (&x)[NC], const int (&lim)[NC], int least,
-                                        int t0, int t1, int stride, int lane)
-{
-    const int P = 1 << c.logT, q = lane >> 4;
-    for (int t = t0; t < t1; t += stride) {
+// Steps t0, t0 + stride, .. below t1 of the columns x, by one wave with a ring of NS steps in LDS of its own: NS - 1 are under way while one is
+// worked on.  start() before the queries are loaded.
+template <int D, int NS> struct Kv4Ring {
+    static constexpr int S = Kv4Stage<D>::LOADS, B = Kv4Stage<D>::BYTES;
+    const Kv4View &c;
+    const char *lds;
+    int s, h, t1, stride, lane;
+    int here;                                   // two bits per step of the ring, the next step's lowest: its tiles that have a page
+    __device__ __forceinline__ void fetch(int slot, int ahead, int t)
+    {
         const Kv4Step st = kv4_step<D>(c, s, h, t, t1);
-        Kv4Keys<D> k[2];
-        Kv4Values<D> v[2];
+        here |= (st.here[0] | st.here[1] << 1) << (2 * ahead);
+        const uint32_t at = lds_address(lds) + slot * B;
 #pragma unroll
-        for (int i = 0; i < 2; i++) k[i].load(st.blk[i], P, st.t[i], lane);
-#pragma unroll
-        for (int i = 0; i < 2; i++) v[i].load(st.blk[i], P, st.t[i], lane);
-        if (t + 32 <= least && st.here[0] && st.here[1]) state.template step<false, LO>(x, k, v, lim, st, t, q);
-        else state.template step<true, LO>(x, k, v, lim, st, t, q);
+        for (int n = 0; n < S; n++) Kv4Stage<D>::load(n, st.blk[0], st.t[0], st.blk[1], st.t[1], 1 << c.logT, at, lane);
     }
-}
+    __device__ __forceinline__ void start(int t0)
+    {
+        here = 0;
+#pragma unroll
+        for (int i = 0; i < NS - 1; i++)
+            if (t0 + i * stride < t1) fetch(i, i, t0 + i * stride);
+    }
+    template <int NC, bool LO>
+    __device__ __forceinline__ void run(Kv4State<D, NC> &state, const Kv4Query<D, LO> (&x)[NC], const int (&lim)[NC], int least, int t0)
+    {
+        int slot = 0;
+        for (int t = t0; t < t1; t += stride) {
+            lds_reads_done();
+            if (t + (NS - 1) * stride < t1) {
+                fetch(slot == 0 ? NS - 1 : slot - 1, NS - 1, t + (NS - 1) * stride);
+                loads_left<(NS - 1) * S>();
+            } else if (NS > 2 && t + (NS - 2) * stride < t1) loads_left<(NS - 2) * S>();
+            else loads_left<0>();
+            const char *stage = lds + slot * B;
+            if (t + 32 <= least && (here & 3) == 3) state.template step<false, LO>(x, stage, lim, here, t, lane);
+            else state.template step<true, LO>(x, stage, lim, here, t, lane);
+            here >>= 2;
+            slot = slot == NS - 1 ? 0 : slot + 1;
+        }
+    }
+};
 
 // what a lane's column is: row and head, tokens it sees (0: a column behind the sequence's last)
 struct Kv4Column { int row, head, lim; };
@@ -651,8 +734,11 @@ template <typename T> __device__ __forceinline__ void kv4_store4(T *p, bool alig
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void kv4_attend_few_kernel(const Kv4Attn a)
 {
-    constexpr int DT = D / 16;
-    __shared__ float os[4][16][D + 4], ms[4][16], ls[4][16];
+    constexpr int DT = D / 16, NS = KV4_RING, RING = NS * Kv4Stage<D>::BYTES;
+    __shared__ __align__(16) char ring[4 * RING];
+    __shared__ float ms[4][16], ls[4][16];
+    float (*os)[16][D + 4] = (float (*)[16][D + 4])ring;    // after the steps: the waves' sums
+    static_assert(sizeof(float[4][16][D + 4]) <= 4 * RING, "the waves' sums fit the rings");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, h = blockIdx.y, chunk = blockIdx.z;
     const Kv4Cols k = kv4_columns<16>(a, blockIdx.x);
     if (k.s < 0) return;
@@ -663,13 +749,16 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_few_kernel(const Kv4Attn a)
     const int most = lanes_max(col.lim), least = lanes_min(live ? col.lim : 1 << 30);
     const int t0 = chunk * a.chunk, t1 = min(most, t0 + a.chunk);
     if (t0 >= t1 && chunk > 0) return;                    // the merge knows from the rows' places
+    Kv4Ring<D, NS> steps = {a.c, ring + wave * RING, k.s, h, t1, 128, lane, 0};
+    steps.start(t0 + 32 * wave);
     Kv4Query<D, sizeof(T) == 4> x[1];
     const T *row = (const T *)a.q + (size_t)col.row * a.q_stride + (size_t)col.head * D;
     x[0].load(row, live, kv4_aligned<T>(a.q, a.q_stride, 8), a.scale, q);
     Kv4State<D, 1> state;
     state.clear();
-    kv4_run(a.c, k.s, h, state, x, lim, least, t0 + 32 * wave, t1, 128, lane);
+    steps.run(state, x, lim, least, t0 + 32 * wave);
     state.finish();
+    __syncthreads();
     if (q == 0) { ms[wave][lane] = state.m[0]; ls[wave][lane] = state.l[0]; }
 #pragma unroll
     for (int j = 0; j < DT; j++) *(f32x4_t *)&os[wave][lane & 15][16 * j + 4 * q] = state.o[0][j];
@@ -709,6 +798,7 @@ template <typename T, int D, int NC>
 __global__ __launch_bounds__(256, 1) void kv4_attend_many_kernel(const Kv4Attn a)
 {
     constexpr int DT = D / 16;
+    __shared__ __align__(16) char ring[8 * Kv4Stage<D>::BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, h = blockIdx.y, chunk = blockIdx.z;
     const Kv4Cols k = kv4_columns<64 * NC>(a, blockIdx.x);
     if (k.s < 0) return;
@@ -729,9 +819,11 @@ __global__ __launch_bounds__(256, 1) void kv4_attend_many_kernel(const Kv4Attn a
     }
     const int t0 = chunk * a.chunk, t1 = min(most, t0 + a.chunk);
     if (t0 >= t1 && chunk > 0) return;
+    Kv4Ring<D, 2> steps = {a.c, ring + wave * 2 * Kv4Stage<D>::BYTES, k.s, h, t1, 32, lane, 0};
+    steps.start(t0);
     Kv4State<D, NC> state;
     state.clear();
-    kv4_run(a.c, k.s, h, state, x, lim, least, t0, t1, 32, lane);
+    steps.run(state, x, lim, least, t0);
     state.finish();
     const bool aligned = kv4_aligned<T>(a.out, a.out_stride, 4);
 #pragma unroll
@@ -812,7 +904,7 @@ __global__ __launch_bounds__(256, 2) void kv4_weights_kernel(const Kv4Attn a)
     Kv4Keys<D> keys[2];
     f16x8_t kk[2][G];
 #pragma unroll
-    for (int i = 0; i < 2; i++) { keys[i].load(st.blk[i], P, st.t[i], lane); keys[i].widen(kk[i]); }
+    for (int i = 0; i < 2; i++) { keys[i].load_page(st.blk[i], P, st.t[i], lane); keys[i].widen(kk[i]); }
     float sum[8] = {};
     const bool aligned = kv4_aligned<T>(a.q, a.q_stride, 8);
     // columns in front of the first that sees token t0 see none of these
