@@ -2653,7 +2653,7 @@ int kg_op_kv4_attention(const kg_kv4_cache *c, int dtype, const void *q, long q_
     if (n_rows > 0) {
         const Kv4Plan p = kv4_plan(c, n_rows, n_heads, max_len);
         const size_t lanes = (size_t)n_rows * n_heads;
-        a.chunk = p.chunk; a.n_chunks = p.n_chunks;
+        a.chunk = p.chunk; a.n_chunks = p.n_chunks; a.shift = p.few ? KV4_SHIFT : KV4_MANY_SHIFT;
         a.part_ml = (float2 *)((char *)work + up(lanes * 4));
         a.part = (float *)((char *)a.part_ml + up(lanes * p.n_chunks * 8));
         const dim3 grid(p.blocks, c->n_kv_heads, p.n_chunks);

@@ -261,14 +261,14 @@ struct Kv4Attn {
     const int *row_start;
     int n_rows, heads, group, max_len;      // group: query heads of a cache head
     int chunk, n_chunks;                    // tokens of a workgroup; of the few-columns kernel a multiple of 128
-    float scale;
+    float scale, shift;                     // shift: the probabilities' factor 2^shift
     const float *w_in;
     float *w_out, *lse;                     // lse [row][head], base 2
     float *part;                            // [row][head][n_chunks][D]: a chunk's sums
     float2 *part_ml;                        // [row][head][n_chunks]: their reference, sum of the probabilities
 };
 
-constexpr float KV4_SHIFT = 28.f;
+constexpr float KV4_SHIFT = 28.f, KV4_MANY_SHIFT = 11.f;
 constexpr int KV4_RING = 3;
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 union Kv4Op { uint32_t w[4]; f16x8_t v; };
@@ -352,7 +352,7 @@ template <int CB> __device__ __forceinline__ Kv4Cols kv4_columns(const Kv4Attn &
 // One column tile's queries: the products' side of the score instructions.  LO: the second part; 16-bit queries are exact without.
 template <int D, bool LO> struct Kv4Query {
     Kv4Op hi[D / 32], lo[LO ? D / 32 : 1], sum;      // slot 2 i, 2 i + 1 of lane group q: components 8 q + i, 8 q + i + 4 of the group
-    float f;                                // what a sum of products is worth as a base-2 exponent
+    float f;                                // what a sum of products is worth as a base-2 exponent: not negative, the scale's sign is in the parts
 
     template <typename T> __device__ __forceinline__ void load(const T *row, bool live, bool aligned, float scale, int q)
     {
@@ -368,14 +368,15 @@ template <int D, bool LO> struct Kv4Query {
         }
         mx = quads_max(mx);
         const int ex = mx > 0.f && mx <= 3.402823466e38f ? __builtin_amdgcn_frexp_expf(mx) : 10;
-        f = __builtin_amdgcn_ldexpf(scale * 1.44269504088896341f, ex - 10);
+        f = __builtin_amdgcn_ldexpf(fabsf(scale) * 1.44269504088896341f, ex - 10);
+        const float sign = scale < 0.f ? -1.f : 1.f;
         uint32_t sh[2] = {0, 0}, sl[2] = {0, 0};
         float total[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int g = 0; g < G; g++) {
             float t = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; e++) { x[g][e] = __builtin_amdgcn_ldexpf(x[g][e], 10 - ex); t += x[g][e]; }
+            for (int e = 0; e < 8; e++) { x[g][e] = __builtin_amdgcn_ldexpf(x[g][e] * sign, 10 - ex); t += x[g][e]; }
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 if (LO) kv4_split(x[g][i], x[g][i + 4], hi[g].w[i], lo[LO ? g : 0].w[i]);
@@ -787,63 +788,334 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_few_kernel(const Kv4Attn a)
             for (int e = 0; e < 4; e++) o[e] = l == 0.f ? 0.f : o[e] / l;
             kv4_store4((T *)a.out + (size_t)kc.row * a.out_stride + (size_t)kc.head * D + d,
                        kv4_aligned<T>(a.out, a.out_stride, 4), o);
-            if (d == 0) a.lse[(size_t)kc.row * a.heads + kc.head] = l == 0.f ? -INFINITY : m - KV4_SHIFT + __builtin_amdgcn_logf(l);
+            if (d == 0) a.lse[(size_t)kc.row * a.heads + kc.head] = l == 0.f ? -INFINITY : m - a.shift + __builtin_amdgcn_logf(l);
         }
     }
 }
 
-// Many columns (prompt rows): a wave takes 16 NC columns over all tokens of a chunk; the four waves of a workgroup read the same tokens
-// at about the same time.
-template <typename T, int D, int NC>
-__global__ __launch_bounds__(256, 1) void kv4_attend_many_kernel(const Kv4Attn a)
+// Many columns (prompt rows): a workgroup takes 64 NC columns of a cache head over the tokens of a chunk, a wave 16 NC of them.  What a step of
+// 32 tokens is multiplied with is made once per workgroup, by all four waves, in LDS: the keys' levels, and the values as two exact fp16
+// parts, n s = n (s's upper 7 bits) + n (its lower 4 bits), so that the probabilities need no group's scale: 8 of them to split into two parts
+// per step and lane and not 8 G, and the minima are one more instruction over the probabilities.  The scores' scales stay a
+// multiplication in fp32.  Steps in which a scale is 4096 or more take a sixteenth of n (15 s would not fit a half) and 16 p.
+// A value scale that is not a number counts as 0 here and makes the outputs of the columns that see it NaN (nan_seen).
+template <int D> struct Kv4Ops {                // byte offsets of a step's operands, 16 bytes a lane each
+    static constexpr int G = D / 32, DT = D / 16, K = 0, VHI = 2 * G * 1024, VLO = VHI + DT * 1024, VM = VLO + DT * 1024, BYTES = VM + 1024;
+};
+struct Kv4Scales { bool big, nan; };            // of a step's value scales: one of 4096 or more, one that is not a number
+
+// tokens of a pair t, t + 1 that count, as a mask of halves
+__device__ __forceinline__ uint32_t kv4_pair_mask(int t, int end) { return (t < end ? 0xffffu : 0u) | (t + 1 < end ? 0xffff0000u : 0u); }
+// end: tokens of the step's tile that count, from its first on
+template <int D> __device__ __forceinline__ Kv4Scales kv4_scales(const char *stage, const int (&end)[2], int lane)
 {
-    constexpr int DT = D / 16;
-    __shared__ __align__(16) char ring[8 * Kv4Stage<D>::BYTES];
+    constexpr int G = D / 32, WORDS = 8 * G;    // of a tile
+    const int l = lane & (2 * WORDS - 1), i = l / WORDS, n = l % WORDS;
+    uint32_t w = *(const uint32_t *)(stage + Kv4Stage<D>::table(i, 2) + 4 * n);
+    w &= kv4_pair_mask(n / (2 * G) * 4 + (n & 1) * 2, i ? end[1] : end[0]) & 0x7fff7fffu;
+    const uint32_t lo = w & 0xffff, hi = w >> 16;
+    Kv4Scales r;
+    r.nan = __any(lo > 0x7c00 || hi > 0x7c00);
+    r.big = __any((lo >= 0x6c00 && lo <= 0x7c00) || (hi >= 0x6c00 && hi <= 0x7c00));
+    return r;
+}
+__device__ __forceinline__ uint32_t kv4_nan_to_zero(uint32_t w)
+{
+    return ((w & 0x7fff) > 0x7c00 ? 0 : w & 0xffff) | ((w >> 16 & 0x7fff) > 0x7c00 ? 0 : w & 0xffff0000u);
+}
+template <int D> __device__ __forceinline__ void kv4_make_ops(const char *stage, char *ops, const int (&end)[2], const Kv4Scales &sc, int wave, int lane)
+{
+    typedef Kv4Stage<D> S;
+    typedef Kv4Ops<D> O;
+    constexpr int G = D / 32, KG = G / 2, VJ = D / 64;      // a wave's operands: KG groups of a tile's keys, VJ of the values
+    const int q = lane >> 4;
+    {
+        const int i = wave >> 1, g0 = (wave & 1) * KG;
+        uint32_t w[KG];
+        lds_read(w, stage + S::k_read(i, lane) + g0 * 4);
+#pragma unroll
+        for (int g = 0; g < KG; g++) {
+            Kv4Op o;
+            kv4_widen(w[g], o.w);
+            *(f16x8_t *)(ops + O::K + (i * G + g0 + g) * 1024 + lane * 16) = o.v;
+        }
+    }
+    const _Float16 c = sc.big ? (_Float16)0.0625f : (_Float16)1.f;
+    const bool part = end[0] < 16 || end[1] < 16;
+    {
+        const int j0 = wave * VJ, g = j0 >> 1, h = j0 >> 2, shift = (j0 & 2) * 4;
+        const f16x2_t c2 = {c, c}, c16 = c2 * f16x2_t{(_Float16)0.0625f, (_Float16)0.0625f};
+        uint32_t w[4], sw[4];
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            uint32_t x[2], y[2];
+            lds_read(x, stage + S::v_read(i, lane) + h * 8);
+            lds_read(y, stage + S::table(i, 2) + (q * G + g) * 8);
+#pragma unroll
+            for (int a = 0; a < 2; a++) { w[2 * i + a] = x[a] >> shift; sw[2 * i + a] = y[a]; }
+        }
+        if (part)
+#pragma unroll
+            for (int a = 0; a < 4; a++) sw[a] &= kv4_pair_mask(4 * q + 2 * (a & 1), end[a >> 1]);
+        if (sc.nan)
+#pragma unroll
+            for (int a = 0; a < 4; a++) sw[a] = kv4_nan_to_zero(sw[a]);
+        f16x2_t hi[4], lo[4];
+#pragma unroll
+        for (int a = 0; a < 4; a++) {
+            hi[a] = __builtin_bit_cast(f16x2_t, sw[a] & 0xfff0fff0u);
+            lo[a] = __builtin_bit_cast(f16x2_t, sw[a]) - hi[a];
+        }
+        auto store = [&](int j, const f16x2_t (&n)[4]) {
+            Kv4Op x, y;
+#pragma unroll
+            for (int a = 0; a < 4; a++) { x.w[a] = __builtin_bit_cast(uint32_t, n[a] * hi[a]); y.w[a] = __builtin_bit_cast(uint32_t, n[a] * lo[a]); }
+            *(f16x8_t *)(ops + O::VHI + j * 1024 + lane * 16) = x.v;
+            *(f16x8_t *)(ops + O::VLO + j * 1024 + lane * 16) = y.v;
+        };
+        f16x2_t n[4];
+        if (VJ == 2 || (wave & 1) == 0) {
+#pragma unroll
+            for (int a = 0; a < 4; a++) n[a] = and_or(w[a], 0x000f000fu, 0x64006400u) * c2 - c2 * f16x2_t{(_Float16)1024, (_Float16)1024};
+            store(j0, n);
+        }
+        if (VJ == 2 || (wave & 1) == 1) {
+#pragma unroll
+            for (int a = 0; a < 4; a++) n[a] = and_or(w[a], 0x00f000f0u, 0x64006400u) * c16 - c2 * f16x2_t{(_Float16)64, (_Float16)64};
+            store(j0 + VJ - 1, n);
+        }
+    }
+    if (wave == 3) {                            // minima: rows are groups
+        const int g = lane & 15;
+        Kv4Op o;
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            uint32_t x[2];
+            lds_read(x, stage + S::table(i, 3) + (q * G + (g & (G - 1))) * 8);
+#pragma unroll
+            for (int a = 0; a < 2; a++) {
+                if (part) x[a] &= kv4_pair_mask(4 * q + 2 * a, end[i]);
+                o.w[2 * i + a] = g < G ? __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, x[a]) * f16x2_t{c, c}) : 0;
+            }
+        }
+        *(f16x8_t *)(ops + O::VM + lane * 16) = o.v;
+    }
+}
+
+template <typename T, int D, int NC>
+__global__ __launch_bounds__(256, 2) void kv4_attend_many_kernel(const Kv4Attn a)
+{
+    constexpr int G = D / 32, DT = D / 16;
+    constexpr bool LO = sizeof(T) == 4;         // fp32 rows: the queries' second part, and the product of both second parts
+    typedef Kv4Stage<D> S;
+    typedef Kv4Ops<D> O;
+    __shared__ __align__(16) char raw[3 * S::BYTES], ops[2 * O::BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, h = blockIdx.y, chunk = blockIdx.z;
-    const Kv4Cols k = kv4_columns<64 * NC>(a, blockIdx.x);
+    const Kv4Cols k = kv4_columns<64 * NC>(a, (int)gridDim.x - 1 - (int)blockIdx.x);       // (late rows, which see most, first)
     if (k.s < 0) return;
-    const int len = kv4_len(a.c, k.s), c0 = k.c0 + wave * 16 * NC;
-    if (c0 >= k.n) return;
-    Kv4Query<D, sizeof(T) == 4> x[NC];
+    const int len = kv4_len(a.c, k.s), c0 = k.c0 + wave * 16 * NC, P = 1 << a.c.logT;
     int lim[NC], most = 0, least = 1 << 30;
-    Kv4Column col[NC];
 #pragma unroll
     for (int n = 0; n < NC; n++) {
         const int cc = c0 + 16 * n + (lane & 15);
-        const bool live = cc < k.n;
-        col[n] = kv4_column(a, k, h, cc, len);
-        lim[n] = col[n].lim;
-        most = max(most, lanes_max(lim[n])); least = min(least, lanes_min(live ? lim[n] : 1 << 30));
-        const T *row = (const T *)a.q + (size_t)col[n].row * a.q_stride + (size_t)col[n].head * D;
-        x[n].load(row, live, kv4_aligned<T>(a.q, a.q_stride, 8), a.scale, q);
+        lim[n] = kv4_column(a, k, h, cc, len).lim;
+        most = max(most, lanes_max(lim[n]));
+        least = min(least, lanes_min(cc < k.n ? lim[n] : 1 << 30));
     }
-    const int t0 = chunk * a.chunk, t1 = min(most, t0 + a.chunk);
+    // the workgroup's last column sees most
+    const Kv4Column end_col = kv4_column(a, k, h, min(k.c0 + 64 * NC, k.n) - 1, len);
+    const int t0 = chunk * a.chunk, t1 = min(__builtin_amdgcn_readfirstlane(end_col.lim), t0 + a.chunk);
     if (t0 >= t1 && chunk > 0) return;
-    Kv4Ring<D, 2> steps = {a.c, ring + wave * 2 * Kv4Stage<D>::BYTES, k.s, h, t1, 32, lane, 0};
-    steps.start(t0);
-    Kv4State<D, NC> state;
-    state.clear();
-    steps.run(state, x, lim, least, t0);
-    state.finish();
+    const uint32_t lds = lds_address(raw);
+    int here = 0;                               // two bits a step: this one's lowest, then the next two's
+    auto fetch = [&](int slot, int ahead, int t) {
+        const Kv4Step st = kv4_step<D>(a.c, k.s, h, t, t1);
+        here |= (st.here[0] | st.here[1] << 1) << (2 * ahead);
+#pragma unroll
+        for (int n = 0; n < S::LOADS; n++)
+            if ((n & 3) == wave) S::load(n, st.blk[0], st.t[0], st.blk[1], st.t[1], P, lds + slot * S::BYTES, lane);
+    };
+    auto ends = [&](int t, int there, int (&e)[2]) {
+#pragma unroll
+        for (int i = 0; i < 2; i++) e[i] = there >> i & 1 ? max(0, min(16, t1 - t - 16 * i)) : 0;
+    };
+    if (t0 < t1) fetch(0, 0, t0);
+    if (t0 + 32 < t1) fetch(1, 1, t0 + 32);
+    Kv4Query<D, LO> x[NC];
+#pragma unroll
+    for (int n = 0; n < NC; n++) {
+        const Kv4Column col = kv4_column(a, k, h, c0 + 16 * n + (lane & 15), len);
+        x[n].load((const T *)a.q + (size_t)col.row * a.q_stride + (size_t)col.head * D, c0 + 16 * n + (lane & 15) < k.n,
+                  kv4_aligned<T>(a.q, a.q_stride, 8), a.scale, q);
+    }
+    f32x4_t o[NC][DT], om[NC];
+    float m[NC], l[NC];
+#pragma unroll
+    for (int n = 0; n < NC; n++) {
+#pragma unroll
+        for (int j = 0; j < DT; j++) o[n][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        om[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        m[n] = -INFINITY; l[n] = 0.f;
+    }
+    loads_left<0>();
+    __syncthreads();
+    if (t0 < t1) {
+        int e[2];
+        ends(t0, here, e);
+        kv4_make_ops<D>(raw, ops, e, kv4_scales<D>(raw, e, lane), wave, lane);
+    }
+    int slot = 0, buf = 0;
+    for (int t = t0; t < t1; t += 32) {
+        // here: this step's operands are made, the next one's numbers are in LDS, and all are done with what stood in the third place
+        lds_reads_done();
+        __syncthreads();
+        const int next = slot == 2 ? 0 : slot + 1;
+        if (t + 64 < t1) fetch(next == 2 ? 0 : next + 1, 2, t + 64);
+        if (t + 32 < t1) {
+            int e[2];
+            ends(t + 32, here >> 2, e);
+            const char *stage = raw + next * S::BYTES;
+            kv4_make_ops<D>(stage, ops + (buf ^ 1) * O::BYTES, e, kv4_scales<D>(stage, e, lane), wave, lane);
+        }
+        if (t < most) {
+            const char *stage = raw + slot * S::BYTES, *op = ops + buf * O::BYTES;
+            int e[2];
+            ends(t, here, e);
+            const Kv4Scales sc = kv4_scales<D>(stage, e, lane);
+            const bool full = t + 32 <= least && e[0] == 16 && e[1] == 16;
+            f32x4_t z[2][NC];
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                uint32_t ks[2 * G], km[G / 2];
+                lds_read(ks, stage + S::table(i, 0) + q * 8 * G);
+                lds_read(km, stage + S::table(i, 1) + (lane & 15) * 2 * G);
+                Kv4Op mm;
+                mm.w[0] = mm.w[2] = km[0];
+                mm.w[1] = mm.w[3] = G == 4 ? km[G / 2 - 1] : 0;
+                const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int n = 0; n < NC; n++) z[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(mm.v, x[n].sum.v, zero, 0, 0, 0);
+#pragma unroll
+                for (int g = 0; g < G; g++) {
+                    const f16x8_t kk = *(const f16x8_t *)(op + O::K + (i * G + g) * 1024 + lane * 16);
+#pragma unroll
+                    for (int n = 0; n < NC; n++) {
+                        f32x4_t d = __builtin_amdgcn_mfma_f32_16x16x32_f16(kk, x[n].hi[g].v, zero, 0, 0, 0);
+                        if (LO) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(kk, x[n].lo[LO ? g : 0].v, d, 0, 0, 0);
+#pragma unroll
+                        for (int j = 0; j < 4; j++) z[i][n][j] = fmaf(half_of(ks[2 * g + (j >> 1)], j & 1), d[j], z[i][n][j]);
+                    }
+                }
+            }
+            KV4_PART;
+            Kv4Op hi[NC], lo[NC];
+#pragma unroll
+            for (int n = 0; n < NC; n++) {
+                float y[8], mx = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 8; j++) {
+                    y[j] = z[j >> 2][n][j & 3];
+                    mx = fmaxf(mx, y[j]);
+                }
+                mx *= x[n].f;
+                if (!full) {
+                    mx = -INFINITY;
+#pragma unroll
+                    for (int j = 0; j < 8; j++) {
+                        const bool see = 4 * q + (j & 3) < e[j >> 2] && t + 16 * (j >> 2) + 4 * q + (j & 3) < lim[n];
+                        y[j] = see ? y[j] * x[n].f : -INFINITY;
+                        mx = fmaxf(mx, y[j]);
+                    }
+                }
+                mx = quads_max(mx);
+                if (__any(mx > m[n])) {
+                    const float m_new = fmaxf(m[n], mx), alpha = __builtin_amdgcn_exp2f(m[n] - (m_new == -INFINITY ? 0.f : m_new));
+#pragma unroll
+                    for (int j = 0; j < DT; j++) o[n][j] *= alpha;
+                    om[n] *= alpha;
+                    l[n] *= alpha;
+                    m[n] = m_new;
+                }
+                const float ref = (m[n] == -INFINITY ? 0.f : m[n]) - a.shift - (sc.big ? 4.f : 0.f), f = full ? x[n].f : 1.f;
+                float p[8];
+#pragma unroll
+                for (int j = 0; j < 8; j++) p[j] = __builtin_amdgcn_exp2f(fmaf(y[j], f, -ref));
+                const float sum = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+                l[n] = fmaf(sum, sc.big ? 0.0625f : 1.f, l[n]);
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) kv4_split(p[j], p[j + 1], hi[n].w[j >> 1], lo[n].w[j >> 1]);
+            }
+            KV4_PART;
+            {
+                const f16x8_t vm = *(const f16x8_t *)(op + O::VM + lane * 16);
+#pragma unroll
+                for (int n = 0; n < NC; n++) {
+                    om[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vm, hi[n].v, om[n], 0, 0, 0);
+                    om[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vm, lo[n].v, om[n], 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < DT; j++) {
+                const f16x8_t vh = *(const f16x8_t *)(op + O::VHI + j * 1024 + lane * 16), vl = *(const f16x8_t *)(op + O::VLO + j * 1024 + lane * 16);
+#pragma unroll
+                for (int n = 0; n < NC; n++) {
+                    o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, hi[n].v, o[n][j], 0, 0, 0);
+                    o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, lo[n].v, o[n][j], 0, 0, 0);
+                    o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vl, hi[n].v, o[n][j], 0, 0, 0);
+                    if (LO) o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vl, lo[n].v, o[n][j], 0, 0, 0);
+                }
+            }
+            if (sc.nan) {                       // a column that sees a group that is not a number has NaN there
+#pragma unroll
+                for (int n = 0; n < NC; n++)
+#pragma unroll
+                    for (int g = 0; g < G; g++) {
+                        float seen = 0.f;
+#pragma nounroll
+                        for (int j = 0; j < 8; j++) {
+                            const bool see = 4 * q + (j & 3) < (j & 4 ? e[1] : e[0]) && t + 16 * (j >> 2) + 4 * q + (j & 3) < lim[n];
+                            const uint32_t w = *(const uint16_t *)(stage + S::table(j >> 2, 2) + (q * G + g) * 8 + (j & 3) * 2);
+                            if (see && (w & 0x7fff) > 0x7c00) seen = 1.f;
+                        }
+                        if (quads_max(seen) > 0.f) om[n][g] = __builtin_nanf("");
+                    }
+            }
+        }
+        loads_left<0>();
+        here >>= 2;
+        slot = next;
+        buf ^= 1;
+    }
     const bool aligned = kv4_aligned<T>(a.out, a.out_stride, 4);
 #pragma unroll
     for (int n = 0; n < NC; n++) {
-        if (c0 + 16 * n + (lane & 15) >= k.n) continue;
-        const float l = state.l[n];
-        if (a.n_chunks > 1) {
-            const size_t at = ((size_t)col[n].row * a.heads + col[n].head) * a.n_chunks + chunk;
+        const float total = quads_sum(l[n]);
+        // the groups' minima stand in the lanes of the first four rows
 #pragma unroll
-            for (int j = 0; j < DT; j++) *(f32x4_t *)(a.part + at * D + 16 * j + 4 * q) = state.o[n][j];
-            if (q == 0) a.part_ml[at] = float2{state.m[n], l};
+        for (int g = 0; g < G; g++) {
+            const float v = __shfl(om[n][g], lane & 15);
+#pragma unroll
+            for (int j = 2 * g; j < 2 * g + 2; j++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) o[n][j][i] += v;
+        }
+        if (c0 + 16 * n + (lane & 15) >= k.n) continue;
+        const Kv4Column col = kv4_column(a, k, h, c0 + 16 * n + (lane & 15), len);
+        if (a.n_chunks > 1) {
+            const size_t at = ((size_t)col.row * a.heads + col.head) * a.n_chunks + chunk;
+#pragma unroll
+            for (int j = 0; j < DT; j++) *(f32x4_t *)(a.part + at * D + 16 * j + 4 * q) = o[n][j];
+            if (q == 0) a.part_ml[at] = float2{m[n], total};
         } else {
-            T *out = (T *)a.out + (size_t)col[n].row * a.out_stride + (size_t)col[n].head * D;
+            T *out = (T *)a.out + (size_t)col.row * a.out_stride + (size_t)col.head * D;
 #pragma unroll
             for (int j = 0; j < DT; j++) {
-                f32x4_t o;
-                for (int i = 0; i < 4; i++) o[i] = l == 0.f ? 0.f : state.o[n][j][i] / l;
-                kv4_store4(out + 16 * j + 4 * q, aligned, o);
+                f32x4_t y;
+#pragma unroll
+                for (int i = 0; i < 4; i++) y[i] = total == 0.f ? 0.f : o[n][j][i] / total;
+                kv4_store4(out + 16 * j + 4 * q, aligned, y);
             }
-            if (q == 0) a.lse[(size_t)col[n].row * a.heads + col[n].head] = l == 0.f ? -INFINITY : state.m[n] - KV4_SHIFT + __builtin_amdgcn_logf(l);
+            if (q == 0) a.lse[(size_t)col.row * a.heads + col.head] = total == 0.f ? -INFINITY : m[n] - a.shift + __builtin_amdgcn_logf(total);
         }
     }
 }
@@ -883,7 +1155,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(const Kv4Attn a)
         const float v = (os[0][threadIdx.x] + os[1][threadIdx.x]) + (os[2][threadIdx.x] + os[3][threadIdx.x]);
         ((T *)a.out)[(size_t)r * a.out_stride + (size_t)hq * D + threadIdx.x] = (T)(total == 0.f ? 0.f : v / total);
     }
-    if (threadIdx.x == 0) a.lse[blockIdx.x] = total == 0.f ? -INFINITY : m - KV4_SHIFT + __builtin_amdgcn_logf(total);
+    if (threadIdx.x == 0) a.lse[blockIdx.x] = total == 0.f ? -INFINITY : m - a.shift + __builtin_amdgcn_logf(total);
 }
 
 // w_out[s][h][t] = w_in + the probabilities of token t, summed over the rows and the query heads of head h.  A wave takes 32 tokens and goes over
