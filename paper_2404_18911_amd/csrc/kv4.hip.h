@@ -368,7 +368,7 @@ template <int D, bool LO> struct Kv4Query {
         }
         mx = quads_max(mx);
         const int ex = mx > 0.f && mx <= 3.402823466e38f ? __builtin_amdgcn_frexp_expf(mx) : 10;
-        f = __builtin_amdgcn_ldexpf(fabsf(scale) * 1.44269504088896341f, ex - 10);
+        f = fmaxf(__builtin_amdgcn_ldexpf(fabsf(scale) * 1.44269504088896341f, ex - 10), 1.17549435e-38f);     // (above 0: a masked score stays -inf)
         const float sign = scale < 0.f ? -1.f : 1.f;
         uint32_t sh[2] = {0, 0}, sl[2] = {0, 0};
         float total[4] = {0.f, 0.f, 0.f, 0.f};
@@ -794,36 +794,52 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_few_kernel(const Kv4Attn a)
 }
 
 // Many columns (prompt rows): a workgroup takes 64 NC columns of a cache head over the tokens of a chunk, a wave 16 NC of them.  What a step of
-// 32 tokens is multiplied with is made once per workgroup, by all four waves, in LDS: the keys' levels, and the values as two exact fp16
-// parts, n s = n (s's upper 7 bits) + n (its lower 4 bits), so that the probabilities need no group's scale: 8 of them to split into two parts
-// per step and lane and not 8 G, and the minima are one more instruction over the probabilities.  The scores' scales stay a
-// multiplication in fp32.  Steps in which a scale is 4096 or more take a sixteenth of n (15 s would not fit a half) and 16 p.
-// A value scale that is not a number counts as 0 here and makes the outputs of the columns that see it NaN (nan_seen).
+// 32 tokens is multiplied with is made once per workgroup, by all four waves, in LDS: the keys' levels (the scores' scales stay a
+// multiplication in fp32), and the values so that the probabilities need no group's scale: 8 of them per step and lane, not 8 G.
+//   fp32 and fp16 rows: the values as two exact fp16 parts, n s = n (s's upper 7 bits) + n (its lower 4 bits), the minima as one more
+//     instruction over the probabilities, these in two parts.  Of the four products fp16 rows leave out that of both second parts (2^-18).
+//   bf16 rows: values s n + m and probabilities rounded to fp16, 2^-11 each of what they are, an eighth of the 2^-8 that the output is rounded by:
+//     half of the matrix instructions and of what is read from LDS.
+// Steps with a scale of 2048 or a minimum of 16384 or more take a sixteenth of the values (they might not fit a half) and 16 p.
+// A value scale that is not a number counts as 0 here and makes the outputs of the columns that see it NaN (nan).
 template <int D> struct Kv4Ops {                // byte offsets of a step's operands, 16 bytes a lane each
-    static constexpr int G = D / 32, DT = D / 16, K = 0, VHI = 2 * G * 1024, VLO = VHI + DT * 1024, VM = VLO + DT * 1024, BYTES = VM + 1024;
+    static constexpr int G = D / 32, DT = D / 16, K = 0, VHI = 2 * G * 1024, VLO = VHI + DT * 1024, VM = VLO + DT * 1024;
+    static constexpr int bytes(bool parts) { return parts ? VM + 1024 : VLO; }
 };
-struct Kv4Scales { bool big, nan; };            // of a step's value scales: one of 4096 or more, one that is not a number
+struct Kv4Scales { bool big, nan; };            // of a step's value scales: big as above, one that is not a number
 
+// Which of a step's tokens count: `left` from its first on, and of those the ones in tiles that have a page (bits of `there`).
+struct Kv4Part {
+    int left, there;
+    __device__ __forceinline__ bool all() const { return left >= 32 && there == 3; }
+    __device__ __forceinline__ int end(int i) const { return there >> i & 1 ? left - 16 * i : 0; }      // of tile i
+};
 // tokens of a pair t, t + 1 that count, as a mask of halves
 __device__ __forceinline__ uint32_t kv4_pair_mask(int t, int end) { return (t < end ? 0xffffu : 0u) | (t + 1 < end ? 0xffff0000u : 0u); }
-// end: tokens of the step's tile that count, from its first on
-template <int D> __device__ __forceinline__ Kv4Scales kv4_scales(const char *stage, const int (&end)[2], int lane)
+template <int D> __device__ __forceinline__ Kv4Scales kv4_scales(const char *stage, const Kv4Part &part, int lane)
 {
     constexpr int G = D / 32, WORDS = 8 * G;    // of a tile
     const int l = lane & (2 * WORDS - 1), i = l / WORDS, n = l % WORDS;
-    uint32_t w = *(const uint32_t *)(stage + Kv4Stage<D>::table(i, 2) + 4 * n);
-    w &= kv4_pair_mask(n / (2 * G) * 4 + (n & 1) * 2, i ? end[1] : end[0]) & 0x7fff7fffu;
-    const uint32_t lo = w & 0xffff, hi = w >> 16;
-    Kv4Scales r;
-    r.nan = __any(lo > 0x7c00 || hi > 0x7c00);
-    r.big = __any((lo >= 0x6c00 && lo <= 0x7c00) || (hi >= 0x6c00 && hi <= 0x7c00));
+    uint32_t w = *(const uint32_t *)(stage + Kv4Stage<D>::table(i, 2) + 4 * n), m = *(const uint32_t *)(stage + Kv4Stage<D>::table(i, 3) + 4 * n);
+    if (!part.all()) {
+        const uint32_t mask = kv4_pair_mask(n / (2 * G) * 4 + (n & 1) * 2, i ? part.end(1) : part.end(0));
+        w &= mask; m &= mask;
+    }
+    // halves as whole numbers: 2048 is 0x6800, 16384 0x7400, infinity 0x7c00 and what is not a number beyond
+    const uint32_t lo = w & 0x7fff, hi = w >> 16 & 0x7fff, ml = m & 0x7fff, mh = m >> 16 & 0x7fff;
+    Kv4Scales r = {false, false};
+    if (__any(max(lo, hi) >= 0x6800 || max(ml, mh) >= 0x7400)) {
+        r.nan = __any(lo > 0x7c00 || hi > 0x7c00);
+        r.big = __any((lo >= 0x6800 && lo <= 0x7c00) || (hi >= 0x6800 && hi <= 0x7c00) || max(ml, mh) >= 0x7400);
+    }
     return r;
 }
 __device__ __forceinline__ uint32_t kv4_nan_to_zero(uint32_t w)
 {
     return ((w & 0x7fff) > 0x7c00 ? 0 : w & 0xffff) | ((w >> 16 & 0x7fff) > 0x7c00 ? 0 : w & 0xffff0000u);
 }
-template <int D> __device__ __forceinline__ void kv4_make_ops(const char *stage, char *ops, const int (&end)[2], const Kv4Scales &sc, int wave, int lane)
+template <int D, bool PARTS>
+__device__ __forceinline__ void kv4_make_ops(const char *stage, char *ops, const Kv4Part &part, const Kv4Scales &sc, int wave, int lane)
 {
     typedef Kv4Stage<D> S;
     typedef Kv4Ops<D> O;
@@ -841,37 +857,49 @@ template <int D> __device__ __forceinline__ void kv4_make_ops(const char *stage,
         }
     }
     const _Float16 c = sc.big ? (_Float16)0.0625f : (_Float16)1.f;
-    const bool part = end[0] < 16 || end[1] < 16;
+    const f16x2_t c2 = {c, c}, c16 = c2 * f16x2_t{(_Float16)0.0625f, (_Float16)0.0625f};
+    const bool all = part.all();
     {
         const int j0 = wave * VJ, g = j0 >> 1, h = j0 >> 2, shift = (j0 & 2) * 4;
-        const f16x2_t c2 = {c, c}, c16 = c2 * f16x2_t{(_Float16)0.0625f, (_Float16)0.0625f};
-        uint32_t w[4], sw[4];
+        uint32_t w[4], sw[4], mw[4];
 #pragma unroll
         for (int i = 0; i < 2; i++) {
-            uint32_t x[2], y[2];
+            uint32_t x[2], y[2], z[2] = {0, 0};
             lds_read(x, stage + S::v_read(i, lane) + h * 8);
             lds_read(y, stage + S::table(i, 2) + (q * G + g) * 8);
+            if (!PARTS) lds_read(z, stage + S::table(i, 3) + (q * G + g) * 8);
 #pragma unroll
-            for (int a = 0; a < 2; a++) { w[2 * i + a] = x[a] >> shift; sw[2 * i + a] = y[a]; }
+            for (int a = 0; a < 2; a++) { w[2 * i + a] = x[a] >> shift; sw[2 * i + a] = y[a]; mw[2 * i + a] = z[a]; }
         }
-        if (part)
+        if (!all)
 #pragma unroll
-            for (int a = 0; a < 4; a++) sw[a] &= kv4_pair_mask(4 * q + 2 * (a & 1), end[a >> 1]);
+            for (int a = 0; a < 4; a++) {
+                const uint32_t mask = kv4_pair_mask(4 * q + 2 * (a & 1), part.end(a >> 1));
+                sw[a] &= mask; mw[a] &= mask;
+            }
         if (sc.nan)
 #pragma unroll
             for (int a = 0; a < 4; a++) sw[a] = kv4_nan_to_zero(sw[a]);
         f16x2_t hi[4], lo[4];
 #pragma unroll
         for (int a = 0; a < 4; a++) {
-            hi[a] = __builtin_bit_cast(f16x2_t, sw[a] & 0xfff0fff0u);
-            lo[a] = __builtin_bit_cast(f16x2_t, sw[a]) - hi[a];
+            if (PARTS) {
+                hi[a] = __builtin_bit_cast(f16x2_t, sw[a] & 0xfff0fff0u);
+                lo[a] = __builtin_bit_cast(f16x2_t, sw[a]) - hi[a];
+            } else {
+                hi[a] = __builtin_bit_cast(f16x2_t, sw[a]);
+                lo[a] = __builtin_bit_cast(f16x2_t, mw[a]) * c2;
+            }
         }
         auto store = [&](int j, const f16x2_t (&n)[4]) {
             Kv4Op x, y;
 #pragma unroll
-            for (int a = 0; a < 4; a++) { x.w[a] = __builtin_bit_cast(uint32_t, n[a] * hi[a]); y.w[a] = __builtin_bit_cast(uint32_t, n[a] * lo[a]); }
+            for (int a = 0; a < 4; a++) {
+                x.w[a] = __builtin_bit_cast(uint32_t, PARTS ? n[a] * hi[a] : n[a] * hi[a] + lo[a]);
+                y.w[a] = __builtin_bit_cast(uint32_t, n[a] * lo[a]);
+            }
             *(f16x8_t *)(ops + O::VHI + j * 1024 + lane * 16) = x.v;
-            *(f16x8_t *)(ops + O::VLO + j * 1024 + lane * 16) = y.v;
+            if (PARTS) *(f16x8_t *)(ops + O::VLO + j * 1024 + lane * 16) = y.v;
         };
         f16x2_t n[4];
         if (VJ == 2 || (wave & 1) == 0) {
@@ -885,7 +913,7 @@ template <int D> __device__ __forceinline__ void kv4_make_ops(const char *stage,
             store(j0 + VJ - 1, n);
         }
     }
-    if (wave == 3) {                            // minima: rows are groups
+    if (PARTS && wave == 3) {                   // minima: rows are groups
         const int g = lane & 15;
         Kv4Op o;
 #pragma unroll
@@ -894,8 +922,8 @@ template <int D> __device__ __forceinline__ void kv4_make_ops(const char *stage,
             lds_read(x, stage + S::table(i, 3) + (q * G + (g & (G - 1))) * 8);
 #pragma unroll
             for (int a = 0; a < 2; a++) {
-                if (part) x[a] &= kv4_pair_mask(4 * q + 2 * a, end[i]);
-                o.w[2 * i + a] = g < G ? __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, x[a]) * f16x2_t{c, c}) : 0;
+                if (!all) x[a] &= kv4_pair_mask(4 * q + 2 * a, part.end(i));
+                o.w[2 * i + a] = g < G ? __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, x[a]) * c2) : 0;
             }
         }
         *(f16x8_t *)(ops + O::VM + lane * 16) = o.v;
@@ -906,10 +934,10 @@ template <typename T, int D, int NC>
 __global__ __launch_bounds__(256, 2) void kv4_attend_many_kernel(const Kv4Attn a)
 {
     constexpr int G = D / 32, DT = D / 16;
-    constexpr bool LO = sizeof(T) == 4;         // fp32 rows: the queries' second part, and the product of both second parts
+    constexpr bool LO = sizeof(T) == 4, PARTS = !std::is_same<T, __bf16>::value;      // LO: fp32 rows, the queries' second part, and the product of both second parts
     typedef Kv4Stage<D> S;
     typedef Kv4Ops<D> O;
-    __shared__ __align__(16) char raw[3 * S::BYTES], ops[2 * O::BYTES];
+    __shared__ __align__(16) char raw[3 * S::BYTES], ops[2 * O::bytes(PARTS)];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, h = blockIdx.y, chunk = blockIdx.z;
     const Kv4Cols k = kv4_columns<64 * NC>(a, (int)gridDim.x - 1 - (int)blockIdx.x);       // (late rows, which see most, first)
     if (k.s < 0) return;
@@ -935,10 +963,6 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_many_kernel(const Kv4Attn a
         for (int n = 0; n < S::LOADS; n++)
             if ((n & 3) == wave) S::load(n, st.blk[0], st.t[0], st.blk[1], st.t[1], P, lds + slot * S::BYTES, lane);
     };
-    auto ends = [&](int t, int there, int (&e)[2]) {
-#pragma unroll
-        for (int i = 0; i < 2; i++) e[i] = there >> i & 1 ? max(0, min(16, t1 - t - 16 * i)) : 0;
-    };
     if (t0 < t1) fetch(0, 0, t0);
     if (t0 + 32 < t1) fetch(1, 1, t0 + 32);
     Kv4Query<D, LO> x[NC];
@@ -959,10 +983,11 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_many_kernel(const Kv4Attn a
     }
     loads_left<0>();
     __syncthreads();
+    Kv4Scales sc = {false, false}, sc_next = sc;
     if (t0 < t1) {
-        int e[2];
-        ends(t0, here, e);
-        kv4_make_ops<D>(raw, ops, e, kv4_scales<D>(raw, e, lane), wave, lane);
+        const Kv4Part part = {t1 - t0, here & 3};
+        sc = kv4_scales<D>(raw, part, lane);
+        kv4_make_ops<D, PARTS>(raw, ops, part, sc, wave, lane);
     }
     int slot = 0, buf = 0;
     for (int t = t0; t < t1; t += 32) {
@@ -972,17 +997,15 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_many_kernel(const Kv4Attn a
         const int next = slot == 2 ? 0 : slot + 1;
         if (t + 64 < t1) fetch(next == 2 ? 0 : next + 1, 2, t + 64);
         if (t + 32 < t1) {
-            int e[2];
-            ends(t + 32, here >> 2, e);
+            const Kv4Part part = {t1 - t - 32, here >> 2 & 3};
             const char *stage = raw + next * S::BYTES;
-            kv4_make_ops<D>(stage, ops + (buf ^ 1) * O::BYTES, e, kv4_scales<D>(stage, e, lane), wave, lane);
+            sc_next = kv4_scales<D>(stage, part, lane);
+            kv4_make_ops<D, PARTS>(stage, ops + (buf ^ 1) * O::bytes(PARTS), part, sc_next, wave, lane);
         }
         if (t < most) {
-            const char *stage = raw + slot * S::BYTES, *op = ops + buf * O::BYTES;
-            int e[2];
-            ends(t, here, e);
-            const Kv4Scales sc = kv4_scales<D>(stage, e, lane);
-            const bool full = t + 32 <= least && e[0] == 16 && e[1] == 16;
+            const char *stage = raw + slot * S::BYTES, *op = ops + buf * O::bytes(PARTS);
+            const Kv4Part part = {t1 - t, here & 3};
+            const bool full = t + 32 <= least && part.all();
             f32x4_t z[2][NC];
 #pragma unroll
             for (int i = 0; i < 2; i++) {
@@ -1013,21 +1036,16 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_many_kernel(const Kv4Attn a
             for (int n = 0; n < NC; n++) {
                 float y[8], mx = -INFINITY;
 #pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    y[j] = z[j >> 2][n][j & 3];
-                    mx = fmaxf(mx, y[j]);
-                }
-                mx *= x[n].f;
-                if (!full) {
-                    mx = -INFINITY;
+                for (int j = 0; j < 8; j++) y[j] = z[j >> 2][n][j & 3];
+                if (!full)
 #pragma unroll
                     for (int j = 0; j < 8; j++) {
-                        const bool see = 4 * q + (j & 3) < e[j >> 2] && t + 16 * (j >> 2) + 4 * q + (j & 3) < lim[n];
-                        y[j] = see ? y[j] * x[n].f : -INFINITY;
-                        mx = fmaxf(mx, y[j]);
+                        const int tok = 4 * q + (j & 3);
+                        y[j] = tok < part.end(j >> 2) && t + 16 * (j >> 2) + tok < lim[n] ? y[j] : -INFINITY;
                     }
-                }
-                mx = quads_max(mx);
+#pragma unroll
+                for (int j = 0; j < 8; j++) mx = fmaxf(mx, y[j]);
+                mx = quads_max(mx * x[n].f);
                 if (__any(mx > m[n])) {
                     const float m_new = fmaxf(m[n], mx), alpha = __builtin_amdgcn_exp2f(m[n] - (m_new == -INFINITY ? 0.f : m_new));
 #pragma unroll
@@ -1036,17 +1054,20 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_many_kernel(const Kv4Attn a
                     l[n] *= alpha;
                     m[n] = m_new;
                 }
-                const float ref = (m[n] == -INFINITY ? 0.f : m[n]) - a.shift - (sc.big ? 4.f : 0.f), f = full ? x[n].f : 1.f;
+                const float ref = (m[n] == -INFINITY ? 0.f : m[n]) - a.shift - (sc.big ? 4.f : 0.f);
                 float p[8];
 #pragma unroll
-                for (int j = 0; j < 8; j++) p[j] = __builtin_amdgcn_exp2f(fmaf(y[j], f, -ref));
+                for (int j = 0; j < 8; j++) p[j] = __builtin_amdgcn_exp2f(fmaf(y[j], x[n].f, -ref));
                 const float sum = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
                 l[n] = fmaf(sum, sc.big ? 0.0625f : 1.f, l[n]);
 #pragma unroll
-                for (int j = 0; j < 8; j += 2) kv4_split(p[j], p[j + 1], hi[n].w[j >> 1], lo[n].w[j >> 1]);
+                for (int j = 0; j < 8; j += 2) {
+                    if (PARTS) kv4_split(p[j], p[j + 1], hi[n].w[j >> 1], lo[n].w[j >> 1]);
+                    else hi[n].w[j >> 1] = __builtin_bit_cast(uint32_t, f16x2_t{(_Float16)p[j], (_Float16)p[j + 1]});
+                }
             }
             KV4_PART;
-            {
+            if (PARTS) {
                 const f16x8_t vm = *(const f16x8_t *)(op + O::VM + lane * 16);
 #pragma unroll
                 for (int n = 0; n < NC; n++) {
@@ -1056,10 +1077,13 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_many_kernel(const Kv4Attn a
             }
 #pragma unroll
             for (int j = 0; j < DT; j++) {
-                const f16x8_t vh = *(const f16x8_t *)(op + O::VHI + j * 1024 + lane * 16), vl = *(const f16x8_t *)(op + O::VLO + j * 1024 + lane * 16);
+                const f16x8_t vh = *(const f16x8_t *)(op + O::VHI + j * 1024 + lane * 16);
+#pragma unroll
+                for (int n = 0; n < NC; n++) o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, hi[n].v, o[n][j], 0, 0, 0);
+                if (!PARTS) continue;
+                const f16x8_t vl = *(const f16x8_t *)(op + O::VLO + j * 1024 + lane * 16);
 #pragma unroll
                 for (int n = 0; n < NC; n++) {
-                    o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, hi[n].v, o[n][j], 0, 0, 0);
                     o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, lo[n].v, o[n][j], 0, 0, 0);
                     o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vl, hi[n].v, o[n][j], 0, 0, 0);
                     if (LO) o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vl, lo[n].v, o[n][j], 0, 0, 0);
@@ -1073,7 +1097,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_many_kernel(const Kv4Attn a
                         float seen = 0.f;
 #pragma nounroll
                         for (int j = 0; j < 8; j++) {
-                            const bool see = 4 * q + (j & 3) < (j & 4 ? e[1] : e[0]) && t + 16 * (j >> 2) + 4 * q + (j & 3) < lim[n];
+                            const bool see = 4 * q + (j & 3) < part.end(j >> 2) && t + 16 * (j >> 2) + 4 * q + (j & 3) < lim[n];
                             const uint32_t w = *(const uint16_t *)(stage + S::table(j >> 2, 2) + (q * G + g) * 8 + (j & 3) * 2);
                             if (see && (w & 0x7fff) > 0x7c00) seen = 1.f;
                         }
@@ -1083,6 +1107,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_many_kernel(const Kv4Attn a
         }
         loads_left<0>();
         here >>= 2;
+        sc = sc_next;
         slot = next;
         buf ^= 1;
     }

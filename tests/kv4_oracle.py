@@ -84,14 +84,16 @@ def token_offsets(H, D, T, h, t):
     return o
 
 
-def attention(q, kq, vq, pos, scale, here=None):
+def attention(q, kq, vq, pos, scale, here=None, halves=False):
     """Rows q [r][heads][D] (float64) over keys / values given as (n, s, m) [len][H][G](32): outputs, tolerance of fp32
     arithmetic (without the output's rounding), probabilities [r][heads][len].  pos[i]: last token that row i sees.
     here [len]: tokens that have a page.
 
     Tolerance: a score is sum q_d (s n + m) scale, whose terms' absolute sum is A.  Both factors are held to 2^-21 or better and
     added in fp32: the score is off by at most A 2^-20, a probability by twice that and its own rounding; products with the
-    values are held to 2^-21, and n terms are added in partial sums of at most 64 + n / 64."""
+    values are held to 2^-21, and n terms are added in partial sums of at most 64 + n / 64.
+    halves: rows of bf16 may take values and probabilities rounded to fp16, 2^-11 of either at most.  With the largest value V that is
+    sum p (1 + 2^-11) v (1 + 2^-11) - sum p v <= (2^-10 + 2^-22) V, an eighth of what rounding V itself to bf16 may cost."""
     r, heads, D = q.shape
     n, H = kq[0].shape[:2]
     g = heads // H
@@ -112,7 +114,7 @@ def attention(q, kq, vq, pos, scale, here=None):
             p = np.exp(z - z.max())
             p /= p.sum()
             A = np.max(Ka[see, h] @ np.abs(q[i, j])) * abs(scale)
-            rel = 2 * A * 2.0 ** -20 + 2.0 ** -20 + (64 + see.sum() / 64) * 2.0 ** -24
+            rel = (2.0 ** -10 + 2.0 ** -22 if halves else 0.0) + 2 * A * 2.0 ** -20 + 2.0 ** -20 + (64 + see.sum() / 64) * 2.0 ** -24
             out[i, j] = p @ V[see, h]
             tol[i, j] = rel * np.repeat(Va[see, h].max(0), 32)
             prob[i, j, see] = p

@@ -192,7 +192,7 @@ def _check_attention(c, kv, q, rows, name, got, scale, max_len=None, here=None, 
             want = tol = np.zeros((r,) + q.shape[1:])
             prob = np.zeros((r, q.shape[1], 0))
         else:
-            want, tol, prob = O.attention(q[at:at + r].astype(np.float64), kv[s][0], kv[s][1], pos, scale, hs)
+            want, tol, prob = O.attention(q[at:at + r].astype(np.float64), kv[s][0], kv[s][1], pos, scale, hs, name == "bf16")
         err = np.abs(got[at:at + r] - want)
         lim = tol + O.HALF_STEP[name] * np.abs(want) + 1e-30
         if name == "f16":
@@ -267,6 +267,27 @@ def test_scales(scale):
     _check_attention(c, kv, q, [2], "f32", c.attend(q, [2], "f32", scale=scale), scale)
 
 
+@pytest.mark.parametrize("name", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rows", [2, 70])
+def test_values_at_both_ends_of_the_halves(name, D, rows):
+    """Scales from the least half to the largest, in one sequence and one step; tokens past the length hold larger ones still."""
+    c = Case(2, D, 16, [160])
+    rng = np.random.default_rng(3)
+    x = [rng.standard_normal((150, 2, D)).astype(np.float32) for _ in range(2)]
+    x[1] *= np.exp(rng.uniform(np.log(1e-6), np.log(2e4), (150, 1, 1))).astype(np.float32)
+    x[1][140] = 65504.0                                       # a constant at the very end
+    x[1][141, :, ::2] = -65504.0                              # the widest group
+    x[1][141, :, 1::2] = 65504.0
+    x[1][142] = np.linspace(32700, 65504, D)
+    x = [O.ROUND[name](np.clip(v, -65504, 65504)) for v in x]
+    c.set_lens([150])
+    c.B.op_kv4_append(c.cache, c.rows(x[0], name), c.rows(x[1], name), c.starts([150]))
+    kv = [(O.quantise(x[0]), O.quantise(x[1]))]
+    q = O.ROUND[name](rng.standard_normal((rows, 4, D)).astype(np.float32))
+    _check_attention(c, kv, q, [rows], name, c.attend(q, [rows], name), D ** -0.5)
+
+
 @pytest.mark.parametrize("size", [1e-30, 1e-4, 1e4, 1e25])
 def test_sizes_of_queries_and_values(size):
     """Queries of any size (the scale takes it back) and values near both ends of the halves."""
@@ -334,18 +355,19 @@ def test_missing_pages_are_seen_by_no_row():
             _check_attention(c, kv, q, rows, "f32", got, 128 ** -0.5, here=here, w=wo.cpu().numpy().astype(np.float64))
 
 
+@pytest.mark.parametrize("name", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("rows", [6, 45])
 @pytest.mark.parametrize("kind", ["k", "v"])
-def test_a_token_that_is_not_finite_shows_only_where_it_is_seen(kind, rows):
+def test_a_token_that_is_not_finite_shows_only_where_it_is_seen(kind, rows, name):
     c = Case(2, 128, 16, [60])
     rng = np.random.default_rng(1)
-    x = [rng.standard_normal((50, 2, 128)).astype(np.float32) for _ in range(2)]
+    x = [O.ROUND[name](rng.standard_normal((50, 2, 128)).astype(np.float32)) for _ in range(2)]
     bad = 50 - 4
     x[kind == "v"][bad, 1, 70] = np.inf
     c.set_lens([50])
-    c.B.op_kv4_append(c.cache, c.rows(x[0], "f32"), c.rows(x[1], "f32"), c.starts([50]))
-    q = rng.standard_normal((rows, 4, 128)).astype(np.float32)
-    got = c.attend(q, [rows], "f32")
+    c.B.op_kv4_append(c.cache, c.rows(x[0], name), c.rows(x[1], name), c.starts([50]))
+    q = O.ROUND[name](rng.standard_normal((rows, 4, 128)).astype(np.float32))
+    got = c.attend(q, [rows], name)
     sees = 50 - rows + np.arange(rows) >= bad
     assert np.isfinite(got[~sees]).all() and np.isfinite(got[:, :2]).all()
     part = got[sees][:, 2:]
@@ -353,8 +375,8 @@ def test_a_token_that_is_not_finite_shows_only_where_it_is_seen(kind, rows):
     # every other row has the numbers it has without that token
     x[kind == "v"][bad, 1, 70] = 0.0
     kv = [(O.quantise(x[0]), O.quantise(x[1]))]
-    want, tol, _ = O.attention(q.astype(np.float64), kv[0][0], kv[0][1], 50 - rows + np.arange(rows), 128 ** -0.5)
-    assert (np.abs(got - want)[~sees] <= tol[~sees] + np.abs(want[~sees]) * 2.0 ** -24).all()
+    want, tol, _ = O.attention(q.astype(np.float64), kv[0][0], kv[0][1], 50 - rows + np.arange(rows), 128 ** -0.5, halves=name == "bf16")
+    assert (np.abs(got - want)[~sees] <= tol[~sees] + np.abs(want[~sees]) * O.HALF_STEP[name]).all()
 
 
 @pytest.mark.parametrize("H,heads,D,n", [(4, 4, 128, 700), (2, 4, 64, 131)])
@@ -511,7 +533,7 @@ def test_a_request_with_a_bounded_cache(name, H, heads, D, T, steps, n_evictions
         got = cur.attend(q, [r], name, max_len=cap, w_in=w, w_out=w)
         state = _model_step(state, xk, xv)
         wn = w.cpu().numpy().astype(np.float64)
-        want, tol, prob = O.attention(q.astype(np.float64), state[0], state[1], n - r + np.arange(r), D ** -0.5)
+        want, tol, prob = O.attention(q.astype(np.float64), state[0], state[1], n - r + np.arange(r), D ** -0.5, halves=name == "bf16")
         assert (np.abs(got - want) <= tol + O.HALF_STEP[name] * np.abs(want)).all(), step
         add = prob.reshape(r, H, heads // H, n).sum((0, 2))
         assert np.allclose(wn[0, :, :n], w_before[0, :, :n] + add, rtol=1e-4, atol=1e-6)
