@@ -2645,14 +2645,18 @@ int kg_op_kv4_attention(const kg_kv4_cache *c, int dtype, const void *q, long q_
     const size_t cap = (size_t)c->max_pages * c->page_tokens, w_bytes = (size_t)c->n_seqs * c->n_kv_heads * cap * 4;
     if (weights_in && weights_in != weights_out && bytes_share(weights_in, w_bytes, weights_out, w_bytes)) return KG_EINVAL;
     if (n_rows == 0 && !weights_out) return KG_OK;
+    if ((size_t)n_rows * n_heads + ((size_t)std::min<size_t>(max_len, cap) / 128 + 1) * c->n_kv_heads * c->n_seqs >= (size_t)1 << 31) return KG_EINVAL;
     Kv4Attn a;
+    memset(&a, 0, sizeof(a));
     a.c = kv4_view(c); a.q = q; a.out = out; a.q_stride = q_stride; a.out_stride = out_stride; a.row_start = row_start; a.n_rows = n_rows;
     a.heads = n_heads; a.group = n_heads / c->n_kv_heads; a.max_len = (int)std::min<size_t>(max_len, cap); a.scale = scale;
     a.w_in = weights_in; a.w_out = weights_out; a.lse = (float *)work;
     hipStream_t s = (hipStream_t)hip_stream;
+    Kv4Plan p = {};
+    const size_t lanes = (size_t)n_rows * n_heads;
+    a.n_chunks = 1;
     if (n_rows > 0) {
-        const Kv4Plan p = kv4_plan(c, n_rows, n_heads, max_len);
-        const size_t lanes = (size_t)n_rows * n_heads;
+        p = kv4_plan(c, n_rows, n_heads, max_len);
         a.chunk = p.chunk; a.n_chunks = p.n_chunks; a.shift = p.few ? KV4_SHIFT : KV4_MANY_SHIFT;
         a.part_ml = (float2 *)((char *)work + up(lanes * 4));
         a.part = (float *)((char *)a.part_ml + up(lanes * p.n_chunks * 8));
@@ -2662,14 +2666,15 @@ int kg_op_kv4_attention(const kg_kv4_cache *c, int dtype, const void *q, long q_
 #define KV4_JOIN(T, D) hipLaunchKernelGGL((kv4_join_kernel<T, D>), dim3((unsigned)lanes), dim3(256), 0, s, a)
         if (p.few) KV4_BY_TYPE_AND_DIM(KV4_FEW, c->head_dim);
         else KV4_BY_TYPE_AND_DIM(KV4_MANY, c->head_dim);
-        if (p.n_chunks > 1) KV4_BY_TYPE_AND_DIM(KV4_JOIN, c->head_dim);
+        if (a.n_chunks > 1 && !weights_out) KV4_BY_TYPE_AND_DIM(KV4_JOIN, c->head_dim);
 #undef KV4_FEW
 #undef KV4_MANY
 #undef KV4_JOIN
     }
     if (weights_out) {
-        const dim3 wgrid((a.max_len + 127) / 128, c->n_kv_heads, c->n_seqs);
-#define KV4_LAUNCH(T, D) hipLaunchKernelGGL((kv4_weights_kernel<T, D>), wgrid, dim3(256), 0, s, a)
+        const int n_join = a.n_chunks > 1 ? (int)lanes : 0, token_blocks = (a.max_len + 127) / 128;
+        const dim3 wgrid((unsigned)(n_join + (size_t)token_blocks * c->n_kv_heads * c->n_seqs));
+#define KV4_LAUNCH(T, D) hipLaunchKernelGGL((kv4_weights_kernel<T, D>), wgrid, dim3(256), 0, s, a, n_join, token_blocks)
         KV4_BY_TYPE_AND_DIM(KV4_LAUNCH, c->head_dim);
 #undef KV4_LAUNCH
     }

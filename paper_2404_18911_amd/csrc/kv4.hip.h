@@ -317,6 +317,15 @@ struct Kv4Cols { int s, c0, n, r0, end; };
 template <int CB> __device__ __forceinline__ Kv4Cols kv4_columns(const Kv4Attn &a, int block)
 {
     const int lane = threadIdx.x & 63;
+    if (a.c.n_seqs == 1) {
+        Kv4Cols k;
+        const int first = a.row_start[0];
+        k.s = 0; k.c0 = block * CB; k.end = a.row_start[1];
+        k.r0 = min(max(first, 0), a.n_rows);
+        k.n = (min(max(k.end, k.r0), a.n_rows) - k.r0) * a.group;
+        if (k.c0 >= k.n) k.s = -1;
+        return k;
+    }
     int done = 0;
     for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) {
         const int s = s0 + lane;
@@ -1145,18 +1154,19 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_many_kernel(const Kv4Attn a
     }
 }
 
+// The chunks of a row that were written: those up to the last token that it sees (its block's other columns may see more).
+__device__ __forceinline__ int kv4_row_chunks(const Kv4Attn &a, int lim) { return max(1, (lim + a.chunk - 1) / a.chunk); }
+
 // Joins the chunks of a row and head, a workgroup each: wave w takes chunks w, w + 4, .., lane j of it the reference and sum of the j-th.
-// Chunks behind the last token that any column of the row's block sees were not written; they end no earlier than the row's own.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void kv4_join_kernel(const Kv4Attn a)
+template <typename T, int D> __device__ __forceinline__ void kv4_join(const Kv4Attn &a, int item, float *lds)
 {
-    __shared__ float os[4][D], ms[4], ls[4];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = blockIdx.x / a.heads, hq = blockIdx.x % a.heads;
+    float (*os)[D] = (float (*)[D])lds, *ms = lds + 4 * D, *ls = ms + 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = item / a.heads, hq = item % a.heads;
     const Kv4Row row = kv4_row(a.c, a.row_start, r);
     if (row.s < 0) return;
-    const int lim = max(0, min(row.pos + 1, a.max_len)), n = max(1, (lim + a.chunk - 1) / a.chunk), mine = (n - wave + 3) / 4;
-    const float2 *ml = a.part_ml + (size_t)blockIdx.x * a.n_chunks;
-    const float *p = a.part + ((size_t)blockIdx.x * a.n_chunks + wave) * D + lane;
+    const int n = kv4_row_chunks(a, max(0, min(row.pos + 1, a.max_len))), mine = (n - wave + 3) / 4;
+    const float2 *ml = a.part_ml + (size_t)item * a.n_chunks;
+    const float *p = a.part + ((size_t)item * a.n_chunks + wave) * D + lane;
     const float2 c = lane < mine ? ml[wave + 4 * lane] : float2{-INFINITY, 0.f};
     float m = wave_max(c.x);
     if (lane == 0) ms[wave] = m;
@@ -1180,19 +1190,52 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(const Kv4Attn a)
         const float v = (os[0][threadIdx.x] + os[1][threadIdx.x]) + (os[2][threadIdx.x] + os[3][threadIdx.x]);
         ((T *)a.out)[(size_t)r * a.out_stride + (size_t)hq * D + threadIdx.x] = (T)(total == 0.f ? 0.f : v / total);
     }
-    if (threadIdx.x == 0) a.lse[blockIdx.x] = total == 0.f ? -INFINITY : m - a.shift + __builtin_amdgcn_logf(total);
+}
+template <typename T, int D> __global__ __launch_bounds__(256) void kv4_join_kernel(const Kv4Attn a)
+{
+    __shared__ float lds[4 * D + 8];
+    kv4_join<T, D>(a, blockIdx.x, lds);
 }
 
-// w_out[s][h][t] = w_in + the probabilities of token t, summed over the rows and the query heads of head h.  A wave takes 32 tokens and goes over
-// all columns; a column's scores are those of the attention, its probabilities 2^(z - lse).
+// One tile of 16 columns in LDS, for all waves of a workgroup.
+template <int D, bool LO> struct Kv4Tile {
+    f16x8_t hi[D / 32][64], lo[LO ? D / 32 : 1][64], sum[64];
+    float f[16], lse[16];
+    int lim[16];
+};
+// base-2 logarithm of a column's sum: from its chunks, where there are several
+__device__ __forceinline__ float kv4_lse(const Kv4Attn &a, size_t item, int lim, int q)
+{
+    if (a.n_chunks == 1) return a.lse[item];
+    const int n = kv4_row_chunks(a, lim);
+    const float2 *ml = a.part_ml + item * a.n_chunks;
+    float m = -INFINITY, l = 0.f;
+    for (int i = q; i < n; i += 4) m = fmaxf(m, ml[i].x);
+    m = quads_max(m);
+    const float ref = m == -INFINITY ? 0.f : m;
+    for (int i = q; i < n; i += 4) l = fmaf(__builtin_amdgcn_exp2f(ml[i].x - ref), ml[i].y, l);
+    l = quads_sum(l);
+    return l == 0.f ? -INFINITY : m - a.shift + __builtin_amdgcn_logf(l);
+}
+
+// What follows the chunks of a call with weights, in one launch: workgroups below n_join join a row and head (none where there is one chunk);
+// the others take 128 tokens of a sequence and cache head, 32 a wave, and go over all columns that see them:
+//     w_out[t] = w_in[t] + sum over the columns of 2^(z - lse), the scores those of the attention.
+// Four tiles of columns at a time are made ready in LDS, one by each wave.
 template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void kv4_weights_kernel(const Kv4Attn a)
+__global__ __launch_bounds__(256, 2) void kv4_weights_kernel(const Kv4Attn a, int n_join, int token_blocks)
 {
     constexpr int G = D / 32;
-    const int s = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 63, q = lane >> 4, P = 1 << a.c.logT;
-    const int t0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * 32;
+    constexpr bool LO = sizeof(T) == 4;
+    __shared__ __align__(16) Kv4Tile<D, LO> tiles[4];
+    if ((int)blockIdx.x < n_join) {
+        kv4_join<T, D>(a, blockIdx.x, (float *)tiles);
+        return;
+    }
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, P = 1 << a.c.logT;
+    const int b = blockIdx.x - n_join, hs = b / token_blocks, h = hs % a.c.H, s = hs / a.c.H, first = (b % token_blocks) * 128, t0 = first + 32 * wave;
     const int len = kv4_len(a.c, s), n = min(len, a.max_len);
-    if (t0 >= n) return;
+    if (first >= n) return;
     Kv4Cols k;
     k.s = s; k.c0 = 0;
     k.r0 = min(max(a.row_start[s], 0), a.n_rows); k.end = a.row_start[s + 1];
@@ -1201,35 +1244,66 @@ __global__ __launch_bounds__(256, 2) void kv4_weights_kernel(const Kv4Attn a)
     Kv4Keys<D> keys[2];
     f16x8_t kk[2][G];
 #pragma unroll
-    for (int i = 0; i < 2; i++) { keys[i].load_page(st.blk[i], P, st.t[i], lane); keys[i].widen(kk[i]); }
+    for (int i = 0; i < 2; i++) keys[i].load_page(st.blk[i], P, st.t[i], lane);
+    const size_t at = ((size_t)s * a.c.H + h) * ((size_t)a.c.max_pages << a.c.logT);
+    float old = 0.f;
+    const int mine = t0 + 16 * (lane >> 2 & 1) + 4 * q + (lane & 3);        // the token whose weight this lane writes, lane % 16 below 8
+    const bool writes = (lane & 8) == 0 && mine < n;
+    if (a.w_in && writes) old = a.w_in[at + mine];
+#pragma unroll
+    for (int i = 0; i < 2; i++) keys[i].widen(kk[i]);
     float sum[8] = {};
-    const bool aligned = kv4_aligned<T>(a.q, a.q_stride, 8);
-    // columns in front of the first that sees token t0 see none of these
-    int first = t0 - (len - k.end + k.r0);
-    first = first > 0 && t0 < n ? min(first, k.n) * a.group : 0;
-    for (int c0 = min(first, k.n) & ~15; c0 < k.n; c0 += 16) {
-        const Kv4Column col = kv4_column(a, k, h, c0 + (lane & 15), len);
-        const bool live = c0 + (lane & 15) < k.n;
-        Kv4Query<D, sizeof(T) == 4> x;
-        x.load((const T *)a.q + (size_t)col.row * a.q_stride + (size_t)col.head * D, live, aligned, a.scale, q);
-        const float lse = live ? a.lse[(size_t)col.row * a.heads + col.head] : 0.f;
+    // columns in front of the first that sees the workgroup's first token see none of its tokens
+    const int row = first - (len - k.end + k.r0);
+    for (int c0 = (row > 0 ? min(row, k.n) * a.group : 0) & ~15; c0 < k.n; c0 += 64) {
+        {
+            const int cc = c0 + 16 * wave + (lane & 15);
+            const Kv4Column col = kv4_column(a, k, h, cc, len);
+            Kv4Query<D, LO> x;
+            x.load((const T *)a.q + (size_t)col.row * a.q_stride + (size_t)col.head * D, cc < k.n, kv4_aligned<T>(a.q, a.q_stride, 8), a.scale, q);
+            const float lse = cc < k.n ? kv4_lse(a, (size_t)col.row * a.heads + col.head, col.lim, q) : 0.f;
+            Kv4Tile<D, LO> &tile = tiles[wave];
+            __syncthreads();                    // (the tiles before these have been read)
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
-            const f32x4_t z = keys[i].scores(kk[i], x);
+            for (int g = 0; g < G; g++) {
+                tile.hi[g][lane] = x.hi[g].v;
+                if (LO) tile.lo[LO ? g : 0][lane] = x.lo[LO ? g : 0].v;
+            }
+            tile.sum[lane] = x.sum.v;
+            if (q == 0) { tile.f[lane] = x.f; tile.lse[lane] = lse; tile.lim[lane] = col.lim; }
+            __syncthreads();
+        }
+#pragma unroll 1
+        for (int i = 0; i < 4 && c0 + 16 * i < k.n; i++) {
+            const Kv4Tile<D, LO> &tile = tiles[i];
+            Kv4Query<D, LO> x;
 #pragma unroll
-            for (int j = 0; j < 4; j++)
-                if (st.here[i] && t0 + 16 * i + 4 * q + j < col.lim) sum[4 * i + j] += __builtin_amdgcn_exp2f(z[j] * x.f - lse);
+            for (int g = 0; g < G; g++) {
+                x.hi[g].v = tile.hi[g][lane];
+                if (LO) x.lo[LO ? g : 0].v = tile.lo[LO ? g : 0][lane];
+            }
+            x.sum.v = tile.sum[lane];
+            const float f = tile.f[lane & 15], lse = tile.lse[lane & 15];
+            const int lim = tile.lim[lane & 15];
+#pragma unroll
+            for (int u = 0; u < 2; u++) {
+                const f32x4_t z = keys[u].scores(kk[u], x);
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(z[j], f, -lse));
+                    sum[4 * u + j] += st.here[u] && t0 + 16 * u + 4 * q + j < lim ? p : 0.f;
+                }
+            }
         }
     }
-    // over the 16 columns of a tile
-#pragma unroll
-    for (int j = 0; j < 8; j++) sum[j] = row_sum(sum[j]);
-    const size_t at = ((size_t)s * a.c.H + h) * ((size_t)a.c.max_pages << a.c.logT);
+    // over the 16 columns of a tile; lane l % 16 = j keeps the sum of token j
+    float total = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; j++) {
-        const int t = t0 + 16 * (j >> 2) + 4 * q + (j & 3);
-        if ((lane & 15) == j && t < n) a.w_out[at + t] = (a.w_in ? a.w_in[at + t] : 0.f) + sum[j];
+        const float v = row_sum(sum[j]);
+        total = (lane & 7) == j ? v : total;
     }
+    if (writes) a.w_out[at + mine] = old + total;
 }
 
 // ---- eviction -----------------------------------------------------------------------------------
