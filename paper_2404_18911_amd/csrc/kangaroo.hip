@@ -2613,7 +2613,7 @@ static Kv4Plan kv4_plan(const kg_kv4_cache *c, int n_rows, int n_heads, int max_
     // every sequence may end in a block that is not full
     p.blocks = (int)std::min<long>(cols, (cols + cb - 1) / cb + std::min(c->n_seqs - 1, n_rows - 1));
     const int unit = 128, units = (len + unit - 1) / unit;
-    const long per_chunk = (long)c->n_kv_heads * (p.few ? c->n_seqs : p.blocks), want = p.few ? 1024 : 512;
+    const long per_chunk = (long)c->n_kv_heads * (p.few ? c->n_seqs : p.blocks), want = p.few && c->n_seqs > 1 ? 1024 : 512;
     const long n = std::min<long>({units, 256, std::max<long>(1, want / per_chunk)});      // (256: a lane of kv4_join_kernel each)
     p.chunk = (int)((units + n - 1) / n) * unit;
     p.n_chunks = (len + p.chunk - 1) / p.chunk;

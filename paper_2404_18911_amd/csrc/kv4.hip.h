@@ -717,17 +717,11 @@ __device__ __forceinline__ Kv4Column kv4_column(const Kv4Attn &a, const Kv4Cols 
     c.lim = live ? max(0, min(len - k.end + c.row + 1, a.max_len)) : 0;
     return c;
 }
-__device__ __forceinline__ int lanes_min(int v)
+// the same for a column that is the wave's
+__device__ __forceinline__ int kv4_row_lim(const Kv4Attn &a, const Kv4Cols &k, int col, int len)
 {
-    for (int o = 1; o < 16; o <<= 1) v = min(v, __shfl_xor(v, o));
-    return __builtin_amdgcn_readfirstlane(v);
+    return max(0, min(len - k.end + k.r0 + col / a.group + 1, a.max_len));
 }
-__device__ __forceinline__ int lanes_max(int v)
-{
-    for (int o = 1; o < 16; o <<= 1) v = max(v, __shfl_xor(v, o));
-    return __builtin_amdgcn_readfirstlane(v);
-}
-
 // outputs d = 16 j + 4 q + 0..3 of a row, from sums over l
 template <typename T> __device__ __forceinline__ void kv4_store4(T *p, bool aligned, f32x4_t v)
 {
@@ -756,7 +750,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_few_kernel(const Kv4Attn a)
     const Kv4Column col = kv4_column(a, k, h, k.c0 + (lane & 15), len);
     const bool live = k.c0 + (lane & 15) < k.n;
     const int lim[1] = {col.lim};
-    const int most = lanes_max(col.lim), least = lanes_min(live ? col.lim : 1 << 30);
+    const int most = kv4_row_lim(a, k, min(k.c0 + 16, k.n) - 1, len), least = kv4_row_lim(a, k, k.c0, len);     // (later columns see no less)
     const int t0 = chunk * a.chunk, t1 = min(most, t0 + a.chunk);
     if (t0 >= t1 && chunk > 0) return;                    // the merge knows from the rows' places
     Kv4Ring<D, NS> steps = {a.c, ring + wave * RING, k.s, h, t1, 128, lane, 0};
@@ -951,17 +945,16 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_many_kernel(const Kv4Attn a
     const Kv4Cols k = kv4_columns<64 * NC>(a, (int)gridDim.x - 1 - (int)blockIdx.x);       // (late rows, which see most, first)
     if (k.s < 0) return;
     const int len = kv4_len(a.c, k.s), c0 = k.c0 + wave * 16 * NC, P = 1 << a.c.logT;
-    int lim[NC], most = 0, least = 1 << 30;
+    int lim[NC];
+    Kv4Column col[NC];
 #pragma unroll
     for (int n = 0; n < NC; n++) {
-        const int cc = c0 + 16 * n + (lane & 15);
-        lim[n] = kv4_column(a, k, h, cc, len).lim;
-        most = max(most, lanes_max(lim[n]));
-        least = min(least, lanes_min(cc < k.n ? lim[n] : 1 << 30));
+        col[n] = kv4_column(a, k, h, c0 + 16 * n + (lane & 15), len);
+        lim[n] = col[n].lim;
     }
-    // the workgroup's last column sees most
-    const Kv4Column end_col = kv4_column(a, k, h, min(k.c0 + 64 * NC, k.n) - 1, len);
-    const int t0 = chunk * a.chunk, t1 = min(__builtin_amdgcn_readfirstlane(end_col.lim), t0 + a.chunk);
+    // what the wave's first and last column see, and the workgroup's last (later columns see no less)
+    const int least = c0 < k.n ? kv4_row_lim(a, k, c0, len) : 0, most = c0 < k.n ? kv4_row_lim(a, k, min(c0 + 16 * NC, k.n) - 1, len) : 0;
+    const int t0 = chunk * a.chunk, t1 = min(kv4_row_lim(a, k, min(k.c0 + 64 * NC, k.n) - 1, len), t0 + a.chunk);
     if (t0 >= t1 && chunk > 0) return;
     const uint32_t lds = lds_address(raw);
     int here = 0;                               // two bits a step: this one's lowest, then the next two's
@@ -1210,9 +1203,11 @@ __device__ __forceinline__ float kv4_lse(const Kv4Attn &a, size_t item, int lim,
     const int n = kv4_row_chunks(a, lim);
     const float2 *ml = a.part_ml + item * a.n_chunks;
     float m = -INFINITY, l = 0.f;
+#pragma unroll 8
     for (int i = q; i < n; i += 4) m = fmaxf(m, ml[i].x);
     m = quads_max(m);
     const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll 8
     for (int i = q; i < n; i += 4) l = fmaf(__builtin_amdgcn_exp2f(ml[i].x - ref), ml[i].y, l);
     l = quads_sum(l);
     return l == 0.f ? -INFINITY : m - a.shift + __builtin_amdgcn_logf(l);
@@ -1256,14 +1251,14 @@ __global__ __launch_bounds__(256, 2) void kv4_weights_kernel(const Kv4Attn a, in
     // columns in front of the first that sees the workgroup's first token see none of its tokens
     const int row = first - (len - k.end + k.r0);
     for (int c0 = (row > 0 ? min(row, k.n) * a.group : 0) & ~15; c0 < k.n; c0 += 64) {
-        {
+        __syncthreads();                        // (the tiles before these have been read)
+        if (c0 + 16 * wave < k.n) {
             const int cc = c0 + 16 * wave + (lane & 15);
             const Kv4Column col = kv4_column(a, k, h, cc, len);
             Kv4Query<D, LO> x;
             x.load((const T *)a.q + (size_t)col.row * a.q_stride + (size_t)col.head * D, cc < k.n, kv4_aligned<T>(a.q, a.q_stride, 8), a.scale, q);
             const float lse = cc < k.n ? kv4_lse(a, (size_t)col.row * a.heads + col.head, col.lim, q) : 0.f;
             Kv4Tile<D, LO> &tile = tiles[wave];
-            __syncthreads();                    // (the tiles before these have been read)
 #pragma unroll
             for (int g = 0; g < G; g++) {
                 tile.hi[g][lane] = x.hi[g].v;
@@ -1271,8 +1266,8 @@ __global__ __launch_bounds__(256, 2) void kv4_weights_kernel(const Kv4Attn a, in
             }
             tile.sum[lane] = x.sum.v;
             if (q == 0) { tile.f[lane] = x.f; tile.lse[lane] = lse; tile.lim[lane] = col.lim; }
-            __syncthreads();
         }
+        __syncthreads();
 #pragma unroll 1
         for (int i = 0; i < 4 && c0 + 16 * i < k.n; i++) {
             const Kv4Tile<D, LO> &tile = tiles[i];
@@ -1330,7 +1325,7 @@ struct Kv4Evict {
 // that one scan over the workgroup ranks a whole segment; the weights come from the L2 again in every pass.  Weights share few exponents,
 // so the histogram is held eight times over (lane % 8) against conflicts.  4096 of 32 heads: 9 us; with digits of 8 bits, one histogram
 // and a serial search of it 36.
-constexpr int KV4_SEG = 32, KV4_COPIES = 8;
+constexpr int KV4_SEG = 32, KV4_COPIES = 8, KV4_BINS = 2048 + 8;      // (8: copies of a digit lie in different banks)
 __device__ __forceinline__ int block_scan(int v, int *tmp, int &total)     // exclusive, 1024 threads; tmp [16]
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -1356,7 +1351,7 @@ __device__ __forceinline__ int block_scan(int v, int *tmp, int &total)     // ex
 
 __global__ __launch_bounds__(1024) void kv4_select_kernel(const Kv4Evict a)
 {
-    __shared__ int hist[2048 * KV4_COPIES], tmp[16], found[2];
+    __shared__ int hist[KV4_COPIES * KV4_BINS], tmp[16], found[2];
     const int s = blockIdx.y, h = blockIdx.x, tid = threadIdx.x;
     const size_t in_cap = (size_t)a.src.max_pages << a.src.logT, out_cap = (size_t)a.dst.max_pages << a.dst.logT;
     const float *w = a.w_in + ((size_t)s * a.src.H + h) * in_cap;       // (in_cap is a multiple of 16, so every row is 16-byte aligned if the first is)
@@ -1388,7 +1383,7 @@ __global__ __launch_bounds__(1024) void kv4_select_kernel(const Kv4Evict a)
     for (int pass = 0; pass < 3; pass++) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass < 2 ? 11 : 10;
         if (!need) break;
-        for (int i = tid; i < 2048 * KV4_COPIES; i += 1024) hist[i] = 0;
+        for (int i = tid; i < KV4_COPIES * KV4_BINS; i += 1024) hist[i] = 0;
         __syncthreads();
         for (int s0 = 0; s0 < n; s0 += seg) {
 #pragma unroll
@@ -1401,7 +1396,7 @@ __global__ __launch_bounds__(1024) void kv4_select_kernel(const Kv4Evict a)
                 for (int e = 0; e < 4; e++) {
                     const uint32_t k = kv4_key(x[e]);
                     if (t + e >= lo && t + e < hi && (pass == 0 || k >> (shift + bits) == prefix >> (shift + bits)))
-                        atomicAdd(&hist[(k >> shift & ((1u << bits) - 1)) * KV4_COPIES + (tid & (KV4_COPIES - 1))], 1);
+                        atomicAdd(&hist[(k >> shift & ((1u << bits) - 1)) + (tid & (KV4_COPIES - 1)) * KV4_BINS], 1);
                 }
             }
         }
@@ -1412,7 +1407,7 @@ __global__ __launch_bounds__(1024) void kv4_select_kernel(const Kv4Evict a)
         for (int e = 0; e < 2; e++) {
             c[e] = 0;
 #pragma unroll
-            for (int j = 0; j < KV4_COPIES; j++) c[e] += hist[(2047 - 2 * tid - e) * KV4_COPIES + j];
+            for (int j = 0; j < KV4_COPIES; j++) c[e] += hist[2047 - 2 * tid - e + j * KV4_BINS];
         }
         int total, above = block_scan(c[0] + c[1], tmp, total);
 #pragma unroll
