@@ -2601,7 +2601,7 @@ static bool kv4_attn_shape_ok(const kg_kv4_cache *c, int n_rows, int n_heads, in
 // How the attention is cut.  Few columns (at most 16 a sequence on average): one workgroup of four waves per cache head, 16 columns and chunk
 // of the tokens.  The chunks follow from the arguments that do not change with the rows, so that a row's sums are cut alike whatever
 // stands beside it.
-struct Kv4Plan { bool few; int blocks, chunk, n_chunks; };
+struct Kv4Plan { bool few; int nv, blocks, chunk, n_chunks; };      // nv: few columns, 4 nv of them a workgroup
 static Kv4Plan kv4_plan(const kg_kv4_cache *c, int n_rows, int n_heads, int max_len)
 {
     Kv4Plan p;
@@ -2609,7 +2609,9 @@ static Kv4Plan kv4_plan(const kg_kv4_cache *c, int n_rows, int n_heads, int max_
     const long cols = (long)n_rows * group;
     const int len = (int)std::min<long>(max_len, (long)c->max_pages * c->page_tokens);
     p.few = cols <= 16L * c->n_seqs;
-    const int cb = p.few ? 16 : KV4_MANY_COLUMNS;
+    // (a wave's work on its scores grows with nv: XXX)
+    p.nv = cols <= 4L * c->n_seqs ? 1 : cols <= 8L * c->n_seqs ? 2 : 4;
+    const int cb = p.few ? 4 * p.nv : KV4_MANY_COLUMNS;
     // every sequence may end in a block that is not full
     p.blocks = (int)std::min<long>(cols, (cols + cb - 1) / cb + std::min(c->n_seqs - 1, n_rows - 1));
     const int unit = 128, units = (len + unit - 1) / unit;
@@ -2661,13 +2663,19 @@ int kg_op_kv4_attention(const kg_kv4_cache *c, int dtype, const void *q, long q_
         a.part_ml = (float2 *)((char *)work + up(lanes * 4));
         a.part = (float *)((char *)a.part_ml + up(lanes * p.n_chunks * 8));
         const dim3 grid(p.blocks, c->n_kv_heads, p.n_chunks);
-#define KV4_FEW(T, D) hipLaunchKernelGGL((kv4_attend_few_kernel<T, D>), grid, dim3(256), 0, s, a)
+#define KV4_FEW1(T, D) hipLaunchKernelGGL((kv4_attend_few_kernel<T, D, 1>), grid, dim3(256), 0, s, a)
+#define KV4_FEW2(T, D) hipLaunchKernelGGL((kv4_attend_few_kernel<T, D, 2>), grid, dim3(256), 0, s, a)
+#define KV4_FEW4(T, D) hipLaunchKernelGGL((kv4_attend_few_kernel<T, D, 4>), grid, dim3(256), 0, s, a)
 #define KV4_MANY(T, D) hipLaunchKernelGGL((kv4_attend_many_kernel<T, D, KV4_MANY_TILES>), grid, dim3(256), 0, s, a)
 #define KV4_JOIN(T, D) hipLaunchKernelGGL((kv4_join_kernel<T, D>), dim3((unsigned)lanes), dim3(256), 0, s, a)
-        if (p.few) KV4_BY_TYPE_AND_DIM(KV4_FEW, c->head_dim);
+        if (p.few && p.nv == 1) KV4_BY_TYPE_AND_DIM(KV4_FEW1, c->head_dim);
+        else if (p.few && p.nv == 2) KV4_BY_TYPE_AND_DIM(KV4_FEW2, c->head_dim);
+        else if (p.few) KV4_BY_TYPE_AND_DIM(KV4_FEW4, c->head_dim);
         else KV4_BY_TYPE_AND_DIM(KV4_MANY, c->head_dim);
         if (a.n_chunks > 1 && !weights_out) KV4_BY_TYPE_AND_DIM(KV4_JOIN, c->head_dim);
-#undef KV4_FEW
+#undef KV4_FEW1
+#undef KV4_FEW2
+#undef KV4_FEW4
 #undef KV4_MANY
 #undef KV4_JOIN
     }

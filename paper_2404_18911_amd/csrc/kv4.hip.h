@@ -269,7 +269,6 @@ struct Kv4Attn {
 };
 
 constexpr float KV4_SHIFT = 28.f, KV4_MANY_SHIFT = 11.f;
-constexpr int KV4_RING = 3;
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 union Kv4Op { uint32_t w[4]; f16x8_t v; };
 
@@ -487,20 +486,6 @@ template <int D> struct Kv4Keys {
         return z;
     }
 };
-// e of the tokens' largest value scales, s < 2^(e - 14) (of garbage: 0..31).  Scales are not negative, so halves compare as whole numbers.
-template <int G> __device__ __forceinline__ void kv4_exponents(const uint32_t (&s)[2 * G], float (&e)[4])
-{
-    typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
-#pragma unroll
-    for (int a = 0; a < 2; a++) {
-        u16x2_t mx = __builtin_bit_cast(u16x2_t, s[a]);
-#pragma unroll
-        for (int g = 1; g < G; g++) mx = __builtin_elementwise_max(mx, __builtin_bit_cast(u16x2_t, s[2 * g + a]));
-        const uint32_t w = __builtin_bit_cast(uint32_t, mx);
-        e[2 * a] = (float)(w >> 10 & 31);
-        e[2 * a + 1] = (float)(w >> 26 & 31);
-    }
-}
 template <int N> __device__ __forceinline__ void lds_read(uint32_t (&x)[N], const char *p)
 {
     __builtin_memcpy(x, __builtin_assume_aligned(p, N >= 4 ? 16 : 4 * N), 4 * N);
@@ -528,141 +513,177 @@ template <int D> __device__ __forceinline__ Kv4Step kv4_step(const Kv4View &c, i
     return st;
 }
 
-template <int D, int NC> struct Kv4State {
-    static constexpr int G = D / 32, DT = D / 16;
-    f32x4_t o[NC][DT];
-    float om[NC][G], m[NC], l[NC];
+// Keeps all four registers of a matrix instruction's result until y, which was computed from it, is there.  The compiler gives the registers of
+// numbers that nobody reads to other values at once, with too short a distance: the instruction's late write then destroyed these (scores of
+// all groups from the third on were wrong).
+__device__ __forceinline__ void whole_until(float &y, const f32x4_t &d) { asm("" : "+v"(y) : "v"(d)); }
+
+// Few columns: a wave's state for 4 NV of them.  The scores' matrix has the columns (queries) as rows and the tokens as columns: column
+// c is row 4 (c % 4) + c / 4, so that lane (q, token) holds the scores of columns q, q + 4, .. (NV of them) with its own token of each tile:
+// with one or four columns no lane computes an exponential or splits a product for a column that is not there.  The probabilities
+// times the values' scales go through LDS (xchg) to the lanes that multiply them: products 2 j, 2 j + 1 of lane group q are tokens 4 q + j of
+// both tiles.
+//   131001 tokens of 32 heads, one column: 158 us with all 16 columns in every lane's registers, XXX here.
+template <int D, int NV> struct Kv4Few {
+    static constexpr int G = D / 32, DT = D / 16, VH = D / 64, C = 4 * NV;
+    static constexpr int XCHG = G * 2 * C * 64;         // bytes: [group][part][column][16 tokens] pairs of halves
+    f32x4_t o[DT];                              // column lane % 16 (modulo C), d = 16 j + 4 q + 0..3
+    float om[NV][G], m[NV], l[NV];              // columns q + 4 i; om and l: the lane's tokens' part
 
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
-        for (int n = 0; n < NC; n++) {
+        for (int j = 0; j < DT; j++) o[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < DT; j++) o[n][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < NV; i++) {
 #pragma unroll
-            for (int g = 0; g < G; g++) om[n][g] = 0.f;
-            m[n] = -INFINITY; l[n] = 0.f;
+            for (int g = 0; g < G; g++) om[i][g] = 0.f;
+            m[i] = -INFINITY; l[i] = 0.f;
         }
     }
-    // One step of 32 tokens from t0 on, its numbers in LDS.  MASK: lim[n] is the number of tokens that the lane's column sees, here: the tiles that
+    // One step of 32 tokens from t0 on, its numbers in LDS.  MASK: lim[i] is the number of tokens that the lane's columns see, here: the tiles that
     // have a page.  Written so that few of the step's numbers are in registers at a time.
     template <bool MASK, bool LO>
-    __device__ __forceinline__ void step(const Kv4Query<D, LO> (&x)[NC], const char *stage, const int (&lim)[NC], int here, int t0, int lane)
+    __device__ __forceinline__ void step(const Kv4Query<D, LO> &x, const float (&f)[NV], const char *stage, char *xchg, const int (&lim)[NV], int here,
+                                         int t0, int lane)
     {
-#pragma clang fp contract(off)                      // (both instances of MASK round alike: a row's bits do not depend on which one it went through)
+#pragma clang fp contract(off)                      // (all instances round alike: a row's bits do not depend on which one it went through)
         typedef Kv4Stage<D> S;
-        const int q = lane >> 4;
-        float z[NC][8], e[8];
+        const int q = lane >> 4, tok = lane & 15;
+        const auto number = [&](int i, int table, int g) {      // of the lane's token in tile i
+            return (float)*(const _Float16 *)(stage + S::table(i, table) + ((tok >> 2) * G + g) * 8 + (tok & 3) * 2);
+        };
+        float z[2][NV];
 #pragma unroll
         for (int i = 0; i < 2; i++) {
             Kv4Keys<D> k;
             k.load(stage, i, lane);
             f16x8_t kk[G];
             k.widen(kk);
+            Kv4Op mm;
+            mm.w[0] = mm.w[2] = k.m[0];
+            mm.w[1] = mm.w[3] = G == 4 ? k.m[G / 2 - 1] : 0;
+            const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+            const f32x4_t zm = __builtin_amdgcn_mfma_f32_16x16x32_f16(x.sum.v, mm.v, zero, 0, 0, 0);
+            float y[NV];
 #pragma unroll
-            for (int n = 0; n < NC; n++) {
-                const f32x4_t zz = k.scores(kk, x[n]);
+            for (int n = 0; n < NV; n++) y[n] = zm[n];
 #pragma unroll
-                for (int j = 0; j < 4; j++) z[n][4 * i + j] = zz[j] * x[n].f;
+            for (int g = 0; g < G; g++) {
+                f32x4_t d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x.hi[g].v, kk[g], zero, 0, 0, 0);
+                if (LO) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x.lo[LO ? g : 0].v, kk[g], d, 0, 0, 0);
+                const float s = number(i, 0, g);
+#pragma unroll
+                for (int n = 0; n < NV; n++) y[n] = fmaf(s, d[n], y[n]);
+                whole_until(y[NV - 1], d);
             }
+            whole_until(y[NV - 1], zm);
+#pragma unroll
+            for (int n = 0; n < NV; n++) z[i][n] = y[n] * f[n];
         }
         KV4_PART;
-        uint32_t vs[2][2 * G];
+        float vs[2][G], e[2];
 #pragma unroll
         for (int i = 0; i < 2; i++) {
-            float ee[4];
-            lds_read(vs[i], stage + S::table(i, 2) + q * 8 * G);
-            kv4_exponents<G>(vs[i], ee);
+            // s < 2^(e - 14) for all groups of the token (of garbage: e is some number).  Scales are not negative: halves compare as whole numbers
+            uint32_t mx = 0;
 #pragma unroll
-            for (int j = 0; j < 4; j++) e[4 * i + j] = ee[j];
+            for (int g = 0; g < G; g++) {
+                const _Float16 v = *(const _Float16 *)(stage + S::table(i, 2) + ((tok >> 2) * G + g) * 8 + (tok & 3) * 2);
+                vs[i][g] = (float)v;
+                mx = max(mx, (uint32_t)__builtin_bit_cast(uint16_t, v));
+            }
+            e[i] = (float)(mx >> 10 & 31);
         }
-        bool see[NC][8];
-        float p[NC][8];
+        bool see[2][NV];
+        float p[2][NV], mx[NV];
+        bool grows = false;
 #pragma unroll
-        for (int n = 0; n < NC; n++) {
-            float mx = -INFINITY;
+        for (int n = 0; n < NV; n++) {
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-                see[n][j] = !MASK || ((here >> (j >> 2) & 1) && t0 + 16 * (j >> 2) + 4 * q + (j & 3) < lim[n]);
-                if (!see[n][j]) z[n][j] = -INFINITY;
-                mx = fmaxf(mx, z[n][j] + e[j]);
+            for (int i = 0; i < 2; i++) {
+                see[i][n] = !MASK || ((here >> i & 1) && t0 + 16 * i + tok < lim[n]);
+                if (!see[i][n]) z[i][n] = -INFINITY;
             }
-            mx = quads_max(mx);
-            if (__any(mx > m[n])) {                 // (where it stays the factor is 1)
-                const float m_new = fmaxf(m[n], mx), alpha = __builtin_amdgcn_exp2f(m[n] - (m_new == -INFINITY ? 0.f : m_new));
+            mx[n] = row_max(fmaxf(z[0][n] + e[0], z[1][n] + e[1]));
+            grows |= mx[n] > m[n];
+        }
+        if (__any(grows)) {                         // (where a column's stays its factor is 1)
+            float alpha[NV], to = 0.f;
 #pragma unroll
-                for (int j = 0; j < DT; j++) o[n][j] *= alpha;
-#pragma unroll
-                for (int g = 0; g < G; g++) om[n][g] *= alpha;
-                l[n] *= alpha;
+            for (int n = 0; n < NV; n++) {
+                const float m_new = fmaxf(m[n], mx[n]);
+                alpha[n] = __builtin_amdgcn_exp2f(m[n] - (m_new == -INFINITY ? 0.f : m_new));
+                l[n] *= alpha[n];
                 m[n] = m_new;
+#pragma unroll
+                for (int g = 0; g < G; g++) om[n][g] *= alpha[n];
+                const float v = __shfl(alpha[n], 16 * (tok & 3));       // of column tok, if that is one of these four
+                to = ((tok & (C - 1)) >> 2) == n ? v : to;
             }
+#pragma unroll
+            for (int j = 0; j < DT; j++) o[j] *= to;
+        }
+#pragma unroll
+        for (int n = 0; n < NV; n++) {
             const float ref = (m[n] == -INFINITY ? 0.f : m[n]) - KV4_SHIFT;
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-                p[n][j] = __builtin_amdgcn_exp2f(z[n][j] - ref);
-                l[n] += p[n][j];
+            for (int i = 0; i < 2; i++) p[i][n] = __builtin_amdgcn_exp2f(z[i][n] - ref);
+            l[n] += p[0][n] + p[1][n];
+#pragma unroll
+            for (int g = 0; g < G; g++) {
+                const float x0 = see[0][n] ? p[0][n] * vs[0][g] : 0.f, x1 = see[1][n] ? p[1][n] * vs[1][g] : 0.f;
+                uint32_t hi, lo;
+                kv4_split(x0, x1, hi, lo);
+                char *at = xchg + ((g * 2) * C + q + 4 * n) * 64 + tok * 4;
+                __builtin_memcpy(__builtin_assume_aligned(at, 4), &hi, 4);         // (not as words: what reads them reads halves, and has to come behind)
+                __builtin_memcpy(__builtin_assume_aligned(at + C * 64, 4), &lo, 4);
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < G; g++) {
+            const float m0 = number(0, 3, g), m1 = number(1, 3, g);
+#pragma unroll
+            for (int n = 0; n < NV; n++) {
+                const float y0 = fmaf(p[0][n], m0, om[n][g]);
+                om[n][g] = see[0][n] ? y0 : om[n][g];
+                const float y1 = fmaf(p[1][n], m1, om[n][g]);
+                om[n][g] = see[1][n] ? y1 : om[n][g];
             }
         }
         KV4_PART;
-        constexpr int VH = D / 64;
         uint32_t vw[2][2 * VH];
 #pragma unroll
         for (int i = 0; i < 2; i++) lds_read(vw[i], stage + S::v_read(i, lane));
 #pragma unroll
         for (int h = 0; h < VH; h++) {
-            uint32_t u[4][4];                       // nibbles i of the halfwords
+            uint32_t u[4][4];                       // token 4 q + j of both tiles: nibbles i
 #pragma unroll
-            for (int a = 0; a < 4; a++) kv4_widen(vw[a >> 1][2 * h + (a & 1)], u[a]);
+            for (int a = 0; a < 2; a++) {
+                const uint32_t w0 = vw[0][2 * h + a], w1 = vw[1][2 * h + a];
+                kv4_widen((w0 & 0xffff) | w1 << 16, u[2 * a]);
+                kv4_widen(w0 >> 16 | (w1 & 0xffff0000u), u[2 * a + 1]);
+            }
 #pragma unroll
             for (int g = 2 * h; g < 2 * h + 2; g++) {
-                uint32_t vm[2][2];
-#pragma unroll
-                for (int i = 0; i < 2; i++) lds_read(vm[i], stage + S::table(i, 3) + (q * G + g) * 8);
-                Kv4Op hi[NC], lo[NC];
-#pragma unroll
-                for (int n = 0; n < NC; n++)
-#pragma unroll
-                    for (int j = 0; j < 8; j += 2) {
-                        const uint32_t sw = vs[j >> 2][2 * g + (j >> 1 & 1)], mw = vm[j >> 2][j >> 1 & 1];
-                        const float x0 = see[n][j] ? fmaf(p[n][j], half_of(sw, 0), 0.f) : 0.f, x1 = see[n][j + 1] ? fmaf(p[n][j + 1], half_of(sw, 1), 0.f) : 0.f;
-                        kv4_split(x0, x1, hi[n].w[j >> 1], lo[n].w[j >> 1]);
-                        const float y0 = fmaf(p[n][j], half_of(mw, 0), om[n][g]);
-                        om[n][g] = see[n][j] ? y0 : om[n][g];
-                        const float y1 = fmaf(p[n][j + 1], half_of(mw, 1), om[n][g]);
-                        om[n][g] = see[n][j + 1] ? y1 : om[n][g];
-                    }
+                Kv4Op hi, lo;
+                const char *at = xchg + ((g * 2) * C + (tok & (C - 1))) * 64 + q * 16;
+                lds_read(hi.w, at);
+                lds_read(lo.w, at + C * 64);
 #pragma unroll
                 for (int j = 2 * g; j < 2 * g + 2; j++) {
                     Kv4Op a;
 #pragma unroll
                     for (int w = 0; w < 4; w++) a.w[w] = u[w][j & 3];
-#pragma unroll
-                    for (int n = 0; n < NC; n++) {
-                        o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, hi[n].v, o[n][j], 0, 0, 0);
-                        o[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, lo[n].v, o[n][j], 0, 0, 0);
-                    }
+                    o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, hi.v, o[j], 0, 0, 0);
+                    o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, lo.v, o[j], 0, 0, 0);
                 }
             }
         }
     }
-    // the minima's part joins the sums, the lanes of a column their parts of the probabilities' sum
-    __device__ __forceinline__ void finish()
-    {
-#pragma unroll
-        for (int n = 0; n < NC; n++) {
-            l[n] = quads_sum(l[n]);
-#pragma unroll
-            for (int g = 0; g < G; g++) om[n][g] = quads_sum(om[n][g]);
-#pragma unroll
-            for (int j = 0; j < DT; j++)
-#pragma unroll
-                for (int i = 0; i < 4; i++) o[n][j][i] += om[n][j >> 1];
-        }
-    }
 };
 
-// Steps t0, t0 + stride, .. below t1 of the columns x, by one wave with a ring of NS steps in LDS of its own: NS - 1 are under way while one is
+// Steps t0, t0 + stride, .. below t1, by one wave with a ring of NS steps in LDS of its own: NS - 1 are under way while one is
 // worked on.  start() before the queries are loaded.
 template <int D, int NS> struct Kv4Ring {
     static constexpr int S = Kv4Stage<D>::LOADS, B = Kv4Stage<D>::BYTES;
@@ -685,8 +706,9 @@ template <int D, int NS> struct Kv4Ring {
         for (int i = 0; i < NS - 1; i++)
             if (t0 + i * stride < t1) fetch(i, i, t0 + i * stride);
     }
-    template <int NC, bool LO>
-    __device__ __forceinline__ void run(Kv4State<D, NC> &state, const Kv4Query<D, LO> (&x)[NC], const int (&lim)[NC], int least, int t0)
+    template <int NV, bool LO>
+    __device__ __forceinline__ void run(Kv4Few<D, NV> &state, const Kv4Query<D, LO> &x, const float (&f)[NV], char *xchg, const int (&lim)[NV], int least,
+                                        int t0)
     {
         int slot = 0;
         for (int t = t0; t < t1; t += stride) {
@@ -697,8 +719,8 @@ template <int D, int NS> struct Kv4Ring {
             } else if (NS > 2 && t + (NS - 2) * stride < t1) loads_left<(NS - 2) * S>();
             else loads_left<0>();
             const char *stage = lds + slot * B;
-            if (t + 32 <= least && (here & 3) == 3) state.template step<false, LO>(x, stage, lim, here, t, lane);
-            else state.template step<true, LO>(x, stage, lim, here, t, lane);
+            if (t + 32 <= least && (here & 3) == 3) state.template step<false, LO>(x, f, stage, xchg, lim, here, t, lane);
+            else state.template step<true, LO>(x, f, stage, xchg, lim, here, t, lane);
             here >>= 2;
             slot = slot == NS - 1 ? 0 : slot + 1;
         }
@@ -734,41 +756,60 @@ template <typename T> __device__ __forceinline__ void kv4_store4(T *p, bool alig
     }
 }
 
-// Few columns: a workgroup takes a chunk of the tokens for one cache head and up to 16 columns, its four waves every fourth step.
-template <typename T, int D>
+// Few columns: a workgroup takes a chunk of the tokens for one cache head and up to 4 NV columns, its four waves every fourth step.  (Rings of three
+// steps, two for 16 columns: two workgroups a compute unit.)
+template <typename T, int D, int NV>
 __global__ __launch_bounds__(256, 2) void kv4_attend_few_kernel(const Kv4Attn a)
 {
-    constexpr int DT = D / 16, NS = KV4_RING, RING = NS * Kv4Stage<D>::BYTES;
-    __shared__ __align__(16) char ring[4 * RING];
-    __shared__ float ms[4][16], ls[4][16];
-    float (*os)[16][D + 4] = (float (*)[16][D + 4])ring;    // after the steps: the waves' sums
-    static_assert(sizeof(float[4][16][D + 4]) <= 4 * RING, "the waves' sums fit the rings");
+    constexpr int G = D / 32, DT = D / 16, C = 4 * NV, NS = NV == 4 ? 2 : 3, RING = NS * Kv4Stage<D>::BYTES, XCHG = Kv4Few<D, NV>::XCHG;
+    constexpr bool LO = sizeof(T) == 4;
+    __shared__ __align__(16) char ring[4 * RING], xchg[4 * XCHG];
+    __shared__ float ms[4][C], ls[4][C], oms[4][C][G];
+    float (*os)[C][D + 4] = (float (*)[C][D + 4])ring;      // after the steps: the waves' sums
+    static_assert(sizeof(float[4][C][D + 4]) <= 4 * RING, "the waves' sums fit the rings");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, h = blockIdx.y, chunk = blockIdx.z;
-    const Kv4Cols k = kv4_columns<16>(a, blockIdx.x);
+    const Kv4Cols k = kv4_columns<C>(a, blockIdx.x);
     if (k.s < 0) return;
     const int len = kv4_len(a.c, k.s);
-    const Kv4Column col = kv4_column(a, k, h, k.c0 + (lane & 15), len);
-    const bool live = k.c0 + (lane & 15) < k.n;
-    const int lim[1] = {col.lim};
-    const int most = kv4_row_lim(a, k, min(k.c0 + 16, k.n) - 1, len), least = kv4_row_lim(a, k, k.c0, len);     // (later columns see no less)
+    const int most = kv4_row_lim(a, k, min(k.c0 + C, k.n) - 1, len), least = kv4_row_lim(a, k, k.c0, len);     // (later columns see no less)
     const int t0 = chunk * a.chunk, t1 = min(most, t0 + a.chunk);
     if (t0 >= t1 && chunk > 0) return;                    // the merge knows from the rows' places
     Kv4Ring<D, NS> steps = {a.c, ring + wave * RING, k.s, h, t1, 128, lane, 0};
     steps.start(t0 + 32 * wave);
-    Kv4Query<D, sizeof(T) == 4> x[1];
-    const T *row = (const T *)a.q + (size_t)col.row * a.q_stride + (size_t)col.head * D;
-    x[0].load(row, live, kv4_aligned<T>(a.q, a.q_stride, 8), a.scale, q);
-    Kv4State<D, 1> state;
-    state.clear();
-    steps.run(state, x, lim, least, t0 + 32 * wave);
-    state.finish();
-    __syncthreads();
-    if (q == 0) { ms[wave][lane] = state.m[0]; ls[wave][lane] = state.l[0]; }
+    // row lane % 16 of the scores' matrix is column (lane % 16) / 4 + 4 (lane % 4)
+    const int c = (lane >> 2 & 3) + 4 * (lane & 3);
+    const bool live = c < C && k.c0 + c < k.n;
+    const Kv4Column col = kv4_column(a, k, h, k.c0 + c, live ? len : 0);
+    Kv4Query<D, LO> x;
+    x.load((const T *)a.q + (size_t)col.row * a.q_stride + (size_t)col.head * D, live, kv4_aligned<T>(a.q, a.q_stride, 8), a.scale, q);
+    // a lane's scores are of columns q, q + 4, ..: rows 4 q, 4 q + 1, ..
+    float f[NV];
+    int lim[NV];
 #pragma unroll
-    for (int j = 0; j < DT; j++) *(f32x4_t *)&os[wave][lane & 15][16 * j + 4 * q] = state.o[0][j];
+    for (int n = 0; n < NV; n++) {
+        f[n] = __shfl(x.f, 4 * q + n);
+        lim[n] = __shfl(live ? col.lim : 0, 4 * q + n);
+    }
+    Kv4Few<D, NV> state;
+    state.clear();
+    steps.run(state, x, f, xchg + wave * XCHG, lim, least, t0 + 32 * wave);
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NV; n++) {
+        const float l = row_sum(state.l[n]);
+        if ((lane & 15) == 0) { ms[wave][q + 4 * n] = state.m[n]; ls[wave][q + 4 * n] = l; }
+#pragma unroll
+        for (int g = 0; g < G; g++) {
+            const float v = row_sum(state.om[n][g]);
+            if ((lane & 15) == 0) oms[wave][q + 4 * n][g] = v;
+        }
+    }
+    if ((lane & 15) < C)
+#pragma unroll
+        for (int j = 0; j < DT; j++) *(f32x4_t *)&os[wave][lane & 15][16 * j + 4 * q] = state.o[j];
     __syncthreads();
     // a thread takes four outputs of a column
-    for (int i = threadIdx.x; i < 16 * (D / 4); i += 256) {
+    for (int i = threadIdx.x; i < C * (D / 4); i += 256) {
         const int cc = i / (D / 4), d = i % (D / 4) * 4;
         if (k.c0 + cc >= k.n) continue;
         const Kv4Column kc = kv4_column(a, k, h, k.c0 + cc, len);
@@ -778,10 +819,10 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_few_kernel(const Kv4Attn a)
         float l = 0.f;
         f32x4_t o = {0.f, 0.f, 0.f, 0.f};
         for (int w = 0; w < 4; w++) {
-            const float f = __builtin_amdgcn_exp2f(ms[w][cc] - ref);
-            l = fmaf(f, ls[w][cc], l);
+            const float fw = __builtin_amdgcn_exp2f(ms[w][cc] - ref), om = oms[w][cc][d >> 5];
+            l = fmaf(fw, ls[w][cc], l);
             const f32x4_t ow = *(const f32x4_t *)&os[w][cc][d];
-            for (int e = 0; e < 4; e++) o[e] = fmaf(f, ow[e], o[e]);
+            for (int e = 0; e < 4; e++) o[e] = fmaf(fw, ow[e] + om, o[e]);
         }
         if (a.n_chunks > 1) {
             const size_t at = ((size_t)kc.row * a.heads + kc.head) * a.n_chunks + chunk;
@@ -789,8 +830,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_few_kernel(const Kv4Attn a)
             if (d == 0) a.part_ml[at] = float2{m, l};
         } else {
             for (int e = 0; e < 4; e++) o[e] = l == 0.f ? 0.f : o[e] / l;
-            kv4_store4((T *)a.out + (size_t)kc.row * a.out_stride + (size_t)kc.head * D + d,
-                       kv4_aligned<T>(a.out, a.out_stride, 4), o);
+            kv4_store4((T *)a.out + (size_t)kc.row * a.out_stride + (size_t)kc.head * D + d, kv4_aligned<T>(a.out, a.out_stride, 4), o);
             if (d == 0) a.lse[(size_t)kc.row * a.heads + kc.head] = l == 0.f ? -INFINITY : m - a.shift + __builtin_amdgcn_logf(l);
         }
     }
