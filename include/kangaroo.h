@@ -417,9 +417,11 @@ int kg_op_stream_read(const void *src_dev, size_t bytes, void *work_dev, void *h
  *                are fp32.  weights_out (may be NULL) [n_seqs][n_kv_heads][max_pages T] floats: for tokens below the sequence's length,
  *                weights_in (NULL: 0) plus the probabilities of the token summed over the call's rows and the heads that share the
  *                cache head; other entries are left alone.  weights_in may be weights_out.  work_dev: kg_op_kv4_work_bytes bytes
- *                (16-byte aligned), of which nothing is kept between calls.  q and out must not overlap.  Results depend on the
- *                arguments alone, bit for bit.  Up to 16 rows x shared heads of a sequence (n_heads / n_kv_heads x rows): a row's bits do
- *                not depend on the other rows of the call, given the same max_len, numbers of heads and n_seqs.
+ *                (16-byte aligned), of which nothing is kept between calls; calls that may run at the same time need one each.  q and out
+ *                must not overlap.  Results depend on the arguments alone, bit for bit.  In calls with n_rows (n_heads / n_kv_heads) <= 16 n_seqs
+ *                a row's bits do not depend on the other rows, given the same max_len, n_heads, n_kv_heads and n_seqs (a verified row is
+ *                the row decoded alone).  Other calls (prompts) cut their sums otherwise, and in bfloat16 take values and probabilities rounded
+ *                to float16: 2^-11 of either, an eighth of the output's own rounding.
  *   kg_op_kv4_evict        keeps n_keep tokens of each sequence and head: the first n_first, the last n_recent and of the others those with
  *                the largest weights (equal: lower token first; NaN largest), in their order, copied from src into the pages of dst
  *                (other pages than src's, which are only read; dst's len_dev is not read: the caller sets it to min(len, n_keep)).

@@ -105,7 +105,7 @@ __device__ __forceinline__ Kv4Levels kv4_levels(float lo, float hi, bool bad)
 }
 // n = clamp(rint((x - m) / s), 0, 15) of the exact quotient.  (x - m) r in fp32 is within 4e-6 of it (three roundings of a number below 16,
 // or beyond the last level), so only what comes as close as 1e-4 to a border is looked at again, in 64 bits, where x - m and n s are exact:
-// one in 5000, against 64 bits for all 65 us instead of 25 for a prompt's 4096 rows of 32 heads.
+// one in 5000 (64 bits for all: 65 us instead of 39 for the append of 4096 rows of 32 heads).
 __device__ __forceinline__ uint32_t kv4_level(float x, const Kv4Levels &l)
 {
     const float t = fminf(fmaxf((x - l.m) * l.r, 0.f), 15.f);
@@ -245,10 +245,10 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(const Kv4View c, T *k, lo
 //
 // A wave takes 16 NC columns, a column being one row and query head of a sequence and cache head, over steps of 32 tokens (two tiles of 16).
 //   scores   z[t][c] = f_c (sum_g s_tg (n_t . q_c)_g + m_tg . (sum of q_c)_g): the levels n are exact in fp16, so a group's 32 products are one
-//            matrix instruction for each of two fp16 parts of the query (scaled by a power of two to below 2^10: the parts hold 22
+//            matrix instruction for each of two fp16 parts of the query (scaled by a power of two to below 2^10: the parts hold 24
 //            bits), its scale a multiplication in fp32; the minima are one more instruction over the groups, whose result the others add to.
 //   softmax  over steps with a running reference M_c, the largest z_t + e_t seen, where the token's value scales are below 2^(e_t - 14):
-//            2^(z - M + 28) s is then below 2^14 whatever the sizes of values and scales, and as two fp16 parts is held to 22 bits
+//            2^(z - M + 28) s is then below 2^14 whatever the sizes of values and scales, and as two fp16 parts is held to 24 bits
 //            and 2^-39 of the largest.
 //   values   o[d][c] = sum_t n_td (p_t s_tg)_c as matrix instructions, the levels again exact; sum_t p_t m_tg in fp32.
 // The scores of a lane (column lane % 16, tokens 4 (lane / 16) + 0..3 of both tiles) are the products' side of the second matrix
@@ -302,13 +302,16 @@ __device__ __forceinline__ void kv4_widen(uint32_t w, uint32_t (&o)[4])
 }
 __device__ __forceinline__ float half_of(uint32_t w, int i) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(i ? w >> 16 : w)); }
 
-// two fp16 parts of a pair of numbers, rounded towards zero (the second takes what the first leaves)
+// A pair of numbers as halves (one instruction), and in two parts, of which the second takes what the first leaves: 2^-24 of the number at
+// most are lost.  (Parts rounded towards zero lose up to 2^-21, all to one side: outputs over 131001 tokens were off by 7.2e-6 instead of XXX.)
+__device__ __forceinline__ uint32_t kv4_halves(float x, float y) { return __builtin_bit_cast(uint32_t, f16x2_t{(_Float16)x, (_Float16)y}); }
 __device__ __forceinline__ void kv4_split(float x, float y, uint32_t &hi, uint32_t &lo)
 {
     float minus;                            // -1 in a register: x - (float)half as one mixed multiply-add, which the compiler would make a conversion and a difference
     asm("v_mov_b32 %0, -1.0" : "=v"(minus));
-    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, y));
-    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(fmaf(half_of(hi, 0), minus, x), fmaf(half_of(hi, 1), minus, y)));
+    asm("" : "+v"(x), "+v"(y));             // (numbers of fp32: a product that the compiler rounds to a half in one go would differ between instances)
+    hi = kv4_halves(x, y);
+    lo = kv4_halves(fmaf(half_of(hi, 0), minus, x), fmaf(half_of(hi, 1), minus, y));
 }
 
 // The columns of a block: sequence, first column, how many of the sequence's there are.
@@ -388,7 +391,7 @@ template <int D, bool LO> struct Kv4Query {
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 if (LO) kv4_split(x[g][i], x[g][i + 4], hi[g].w[i], lo[LO ? g : 0].w[i]);
-                else hi[g].w[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x[g][i], x[g][i + 4]));
+                else hi[g].w[i] = kv4_halves(x[g][i], x[g][i + 4]);
             }
             total[g] = quads_sum(t);
         }
@@ -523,7 +526,7 @@ __device__ __forceinline__ void whole_until(float &y, const f32x4_t &d) { asm(""
 // with one or four columns no lane computes an exponential or splits a product for a column that is not there.  The probabilities
 // times the values' scales go through LDS (xchg) to the lanes that multiply them: products 2 j, 2 j + 1 of lane group q are tokens 4 q + j of
 // both tiles.
-//   131001 tokens of 32 heads, one column: 158 us with all 16 columns in every lane's registers, XXX here.
+//   One row of 32 heads over 131001 tokens (671 MB): 130 us, 5.2 TB/s (a plain read of memory: 6.5); 158 where every lane held 16 columns.
 template <int D, int NV> struct Kv4Few {
     static constexpr int G = D / 32, DT = D / 16, VH = D / 64, C = 4 * NV;
     static constexpr int XCHG = G * 2 * C * 64;         // bytes: [group][part][column][16 tokens] pairs of halves
@@ -1105,7 +1108,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_many_kernel(const Kv4Attn a
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {
                     if (PARTS) kv4_split(p[j], p[j + 1], hi[n].w[j >> 1], lo[n].w[j >> 1]);
-                    else hi[n].w[j >> 1] = __builtin_bit_cast(uint32_t, f16x2_t{(_Float16)p[j], (_Float16)p[j + 1]});
+                    else hi[n].w[j >> 1] = kv4_halves(p[j], p[j + 1]);
                 }
             }
             KV4_PART;
@@ -1363,7 +1366,7 @@ struct Kv4Evict {
 // Which tokens of a sequence and head stay: radix selection of the need-th largest weight (digits of 11, 11 and 10 bits), then the tokens
 // in order with their ranks.  One workgroup per sequence and head.  A thread takes consecutive tokens, up to 32 of a segment of 32768, so
 // that one scan over the workgroup ranks a whole segment; the weights come from the L2 again in every pass.  Weights share few exponents,
-// so the histogram is held eight times over (lane % 8) against conflicts.  4096 of 32 heads: 9 us; with digits of 8 bits, one histogram
+// so the histogram is held eight times over (lane % 8) against conflicts.  4096 of 32 heads: 16 us; with digits of 8 bits, one histogram
 // and a serial search of it 36.
 constexpr int KV4_SEG = 32, KV4_COPIES = 8, KV4_BINS = 2048 + 8;      // (8: copies of a digit lie in different banks)
 __device__ __forceinline__ int block_scan(int v, int *tmp, int &total)     // exclusive, 1024 threads; tmp [16]

@@ -249,6 +249,33 @@ def test_attention_and_weights(name, H, heads, D, T, lens, rows):
     assert np.array_equal(odd, got)
 
 
+@pytest.mark.parametrize("heads,seed", [(1, 0), (4, 1), (20, 2)])
+def test_many_sequences(heads, seed):
+    """More sequences than lanes, some empty, some without rows; 1, 4 and 20 columns for a row."""
+    rng = np.random.default_rng(seed)
+    lens = [int(x) for x in rng.integers(0, 60, 150)]
+    rows = [int(min(n, r)) if n else int(r > 2) for n, r in zip(lens, rng.integers(0, 4, 150))]
+    c = Case(1, 64, 16, [n + 1 for n in lens], seed=3)
+    kv = c.fill(lens)
+    q = rng.standard_normal((sum(rows), heads, 64)).astype(np.float32)
+    wo = c.torch.full((150, 1, c.cache.capacity), -3.0, device=c.dev)
+    got = c.attend(q, rows, "f32", w_out=wo)
+    _check_attention(c, kv, q, rows, "f32", got, 0.125, w=wo.cpu().numpy().astype(np.float64))
+
+
+@pytest.mark.parametrize("H,heads", [(1, 1), (3, 3), (40, 40)])
+def test_a_cache_longer_than_its_chunks(H, heads):
+    """Long contexts of one, few and many heads: up to 256 chunks are joined."""
+    c = Case(H, 64, 128, [40000 if H == 1 else 6000])
+    n = 39990 if H == 1 else 5990
+    kv = c.fill([n])
+    q = np.random.default_rng(0).standard_normal((1, heads, 64)).astype(np.float32) * 2
+    wo = c.torch.full((1, H, c.cache.capacity), -3.0, device=c.dev)
+    got = c.attend(q, [1], "f32", w_out=wo)
+    _check_attention(c, kv, q, [1], "f32", got, 0.125, w=wo.cpu().numpy().astype(np.float64))
+    assert np.array_equal(c.attend(q, [1], "f32"), got)        # the join alone, and the join beside the weights
+
+
 def test_attention_long_with_a_bound_on_the_length():
     c = Case(2, 128, 128, [9000])
     kv = c.fill([9000])

@@ -44,7 +44,7 @@ def test_append_and_read_refusals():
     L, c, p = B.lib(), _cache(), 1 << 20
     for fn in (L.kg_op_kv4_append, L.kg_op_kv4_read):
         good = [c, 1, p, 512, 2 * p, 512, p, 3, None]
-        for i, v in ((0, None), (1, 3), (1, -1), (2, None), (2, p + 1), (3, 511), (3, -512), (4, None), (4, p + 1), (5, 100), (6, None), (7, -1)):
+        for i, v in ((0, None), (1, 3), (1, -1), (2, None), (2, p + 1), (3, 511), (3, -512), (3, 1 << 45), (3, 1 << 62), (4, None), (4, p + 1), (5, 100), (6, None), (7, -1)):
             a = list(good)
             a[i] = v
             assert fn(*a) == B.KG_EINVAL, (i, v)
