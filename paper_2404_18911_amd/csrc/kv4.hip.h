@@ -290,10 +290,11 @@ __device__ __forceinline__ f16x2_t and_or(uint32_t w, uint32_t mask, uint32_t bi
     asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(w), "s"(mask), "v"(bits));
     return __builtin_bit_cast(f16x2_t, r);
 }
-// levels i and i + 4 of a word as halves, i = 0..3: 1024 + n, or 1024 + 16 n of the nibble above, less what is too much
-__device__ __forceinline__ void kv4_widen(uint32_t w, uint32_t (&o)[4])
+// levels i and i + 4 of a word as halves, less CENTRE, i = 0..3: 1024 + n, or 1024 + 16 n of the nibble above, less what is too much
+template <int CENTRE = 0> __device__ __forceinline__ void kv4_widen(uint32_t w, uint32_t (&o)[4])
 {
-    const f16x2_t one = {(_Float16)1024, (_Float16)1024}, sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f}, sixty_four = {(_Float16)64, (_Float16)64};
+    const f16x2_t one = {(_Float16)(1024 + CENTRE), (_Float16)(1024 + CENTRE)}, sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
+    const f16x2_t sixty_four = {(_Float16)(64 + CENTRE), (_Float16)(64 + CENTRE)};
     const uint32_t hi = w >> 8;
     o[0] = __builtin_bit_cast(uint32_t, and_or(w, 0x000f000fu, 0x64006400u) - one);
     o[1] = __builtin_bit_cast(uint32_t, and_or(w, 0x00f000f0u, 0x64006400u) * sixteenth - sixty_four);
@@ -303,7 +304,7 @@ __device__ __forceinline__ void kv4_widen(uint32_t w, uint32_t (&o)[4])
 __device__ __forceinline__ float half_of(uint32_t w, int i) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(i ? w >> 16 : w)); }
 
 // A pair of numbers as halves (one instruction), and in two parts, of which the second takes what the first leaves: 2^-24 of the number at
-// most are lost.  (Parts rounded towards zero lose up to 2^-21, all to one side: outputs over 131001 tokens were off by 7.2e-6 instead of XXX.)
+// most are lost.  (Parts rounded towards zero lose up to 2^-21, all to one side: outputs over 131001 tokens were off by 7.2e-6 instead of 2.1e-6.)
 __device__ __forceinline__ uint32_t kv4_halves(float x, float y) { return __builtin_bit_cast(uint32_t, f16x2_t{(_Float16)x, (_Float16)y}); }
 __device__ __forceinline__ void kv4_split(float x, float y, uint32_t &hi, uint32_t &lo)
 {
@@ -365,7 +366,8 @@ template <int D, bool LO> struct Kv4Query {
     Kv4Op hi[D / 32], lo[LO ? D / 32 : 1], sum;      // slot 2 i, 2 i + 1 of lane group q: components 8 q + i, 8 q + i + 4 of the group
     float f;                                // what a sum of products is worth as a base-2 exponent: not negative, the scale's sign is in the parts
 
-    template <typename T> __device__ __forceinline__ void load(const T *row, bool live, bool aligned, float scale, int q)
+    // CENTRE: the first parts of the sums in lane group 1 too, against the second parts of m + 8 s (Kv4Ops)
+    template <bool CENTRE = false, typename T> __device__ __forceinline__ void load(const T *row, bool live, bool aligned, float scale, int q)
     {
         constexpr int G = D / 32;
         float x[G][8], mx = 0.f;
@@ -397,7 +399,7 @@ template <int D, bool LO> struct Kv4Query {
         }
         kv4_split(total[0], total[1], sh[0], sl[0]);
         kv4_split(total[2], total[3], sh[1], sl[1]);
-        sum.w[0] = q == 0 ? sh[0] : 0; sum.w[1] = q == 0 ? sh[1] : 0;       // groups 0..3 against the minima's slots 0..3 and 4..7
+        sum.w[0] = q <= (CENTRE ? 1 : 0) ? sh[0] : 0; sum.w[1] = q <= (CENTRE ? 1 : 0) ? sh[1] : 0;       // groups 0..3 against the minima's slots 0..3 and 4..7
         sum.w[2] = q == 0 ? sl[0] : 0; sum.w[3] = q == 0 ? sl[1] : 0;
     }
 };
@@ -844,13 +846,15 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_few_kernel(const Kv4Attn a)
 // multiplication in fp32), and the values so that the probabilities need no group's scale: 8 of them per step and lane, not 8 G.
 //   fp32 and fp16 rows: the values as two exact fp16 parts, n s = n (s's upper 7 bits) + n (its lower 4 bits), the minima as one more
 //     instruction over the probabilities, these in two parts.  Of the four products fp16 rows leave out that of both second parts (2^-18).
+//     Levels are counted from the eighth, minima from there too (m + 8 s, in two parts): the sums that nearly cancel are half as large, and so is
+//     the error (scores off by 4.7e-6 instead of 9.6e-6, 30 their size; 6.1e-6 where keys are widened first and then multiplied in fp32).
 //   bf16 rows: values s n + m and probabilities rounded to fp16, 2^-11 each of what they are, an eighth of the 2^-8 that the output is rounded by:
 //     half of the matrix instructions and of what is read from LDS.
 // Steps with a scale of 2048 or a minimum of 16384 or more take a sixteenth of the values (they might not fit a half) and 16 p.
 // A value scale that is not a number counts as 0 here and makes the outputs of the columns that see it NaN (nan).
 template <int D> struct Kv4Ops {                // byte offsets of a step's operands, 16 bytes a lane each
-    static constexpr int G = D / 32, DT = D / 16, K = 0, VHI = 2 * G * 1024, VLO = VHI + DT * 1024, VM = VLO + DT * 1024;
-    static constexpr int bytes(bool parts) { return parts ? VM + 1024 : VLO; }
+    static constexpr int G = D / 32, DT = D / 16, K = 0, VHI = 2 * G * 1024, VLO = VHI + DT * 1024, VM = VLO + DT * 1024, KM = VM + 1024;
+    static constexpr int bytes(bool parts) { return parts ? KM + 2 * 1024 : VLO; }
 };
 struct Kv4Scales { bool big, nan; };            // of a step's value scales: big as above, one that is not a number
 
@@ -898,7 +902,7 @@ __device__ __forceinline__ void kv4_make_ops(const char *stage, char *ops, const
 #pragma unroll
         for (int g = 0; g < KG; g++) {
             Kv4Op o;
-            kv4_widen(w[g], o.w);
+            kv4_widen<PARTS ? 8 : 0>(w[g], o.w);
             *(f16x8_t *)(ops + O::K + (i * G + g0 + g) * 1024 + lane * 16) = o.v;
         }
     }
@@ -950,29 +954,54 @@ __device__ __forceinline__ void kv4_make_ops(const char *stage, char *ops, const
         f16x2_t n[4];
         if (VJ == 2 || (wave & 1) == 0) {
 #pragma unroll
-            for (int a = 0; a < 4; a++) n[a] = and_or(w[a], 0x000f000fu, 0x64006400u) * c2 - c2 * f16x2_t{(_Float16)1024, (_Float16)1024};
+            for (int a = 0; a < 4; a++) n[a] = and_or(w[a], 0x000f000fu, 0x64006400u) * c2 - c2 * f16x2_t{(_Float16)(PARTS ? 1032 : 1024), (_Float16)(PARTS ? 1032 : 1024)};
             store(j0, n);
         }
         if (VJ == 2 || (wave & 1) == 1) {
 #pragma unroll
-            for (int a = 0; a < 4; a++) n[a] = and_or(w[a], 0x00f000f0u, 0x64006400u) * c16 - c2 * f16x2_t{(_Float16)64, (_Float16)64};
+            for (int a = 0; a < 4; a++) n[a] = and_or(w[a], 0x00f000f0u, 0x64006400u) * c16 - c2 * f16x2_t{(_Float16)(PARTS ? 72 : 64), (_Float16)(PARTS ? 72 : 64)};
             store(j0 + VJ - 1, n);
         }
     }
-    if (PARTS && wave == 3) {                   // minima: rows are groups
-        const int g = lane & 15;
+    if (PARTS && wave == 3) {                   // minima of the values: rows are groups, first parts, then the second ones
+        const int g = lane & (G - 1), row = lane & 15;
         Kv4Op o;
 #pragma unroll
         for (int i = 0; i < 2; i++) {
-            uint32_t x[2];
-            lds_read(x, stage + S::table(i, 3) + (q * G + (g & (G - 1))) * 8);
+            uint32_t x[2], y[2];
+            lds_read(x, stage + S::table(i, 3) + (q * G + g) * 8);
+            lds_read(y, stage + S::table(i, 2) + (q * G + g) * 8);
 #pragma unroll
             for (int a = 0; a < 2; a++) {
-                if (!all) x[a] &= kv4_pair_mask(4 * q + 2 * a, part.end(i));
-                o.w[2 * i + a] = g < G ? __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, x[a]) * c2) : 0;
+                if (!all) {
+                    const uint32_t mask = kv4_pair_mask(4 * q + 2 * a, part.end(i));
+                    x[a] &= mask; y[a] &= mask;
+                }
+                if (sc.nan) y[a] = kv4_nan_to_zero(y[a]);
+                uint32_t hi, lo;
+                kv4_split(fmaf(half_of(y[a], 0), 8.f, half_of(x[a], 0)) * (float)c, fmaf(half_of(y[a], 1), 8.f, half_of(x[a], 1)) * (float)c, hi, lo);
+                o.w[2 * i + a] = row < G ? hi : row < 2 * G ? lo : 0;
             }
         }
         *(f16x8_t *)(ops + O::VM + lane * 16) = o.v;
+    }
+    if (PARTS && wave < 2) {                    // minima of tile `wave`'s keys: first parts against both of the sums' (lane group 0), second against the first (1)
+        const int tok = lane & 15;
+        uint32_t km[G / 2], hi[2] = {0, 0}, lo[2] = {0, 0};
+        lds_read(km, stage + S::table(wave, 1) + tok * 2 * G);
+#pragma unroll
+        for (int g = 0; g < G; g += 2) {
+            const char *ks = stage + S::table(wave, 0) + ((tok >> 2) * G + g) * 8 + (tok & 3) * 2;
+            kv4_split(fmaf((float)*(const _Float16 *)ks, 8.f, half_of(km[g / 2], 0)), fmaf((float)*(const _Float16 *)(ks + 8), 8.f, half_of(km[g / 2], 1)),
+                      hi[g / 2], lo[g / 2]);
+        }
+        Kv4Op o;
+#pragma unroll
+        for (int g = 0; g < 2; g++) {
+            o.w[g] = q == 0 ? hi[g] : q == 1 ? lo[g] : 0;
+            o.w[2 + g] = q == 0 ? hi[g] : 0;
+        }
+        *(f16x8_t *)(ops + O::KM + wave * 1024 + lane * 16) = o.v;
     }
 }
 
@@ -1014,7 +1043,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_many_kernel(const Kv4Attn a
 #pragma unroll
     for (int n = 0; n < NC; n++) {
         const Kv4Column col = kv4_column(a, k, h, c0 + 16 * n + (lane & 15), len);
-        x[n].load((const T *)a.q + (size_t)col.row * a.q_stride + (size_t)col.head * D, c0 + 16 * n + (lane & 15) < k.n,
+        x[n].template load<PARTS>((const T *)a.q + (size_t)col.row * a.q_stride + (size_t)col.head * D, c0 + 16 * n + (lane & 15) < k.n,
                   kv4_aligned<T>(a.q, a.q_stride, 8), a.scale, q);
     }
     f32x4_t o[NC][DT], om[NC];
@@ -1054,12 +1083,16 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_many_kernel(const Kv4Attn a
             f32x4_t z[2][NC];
 #pragma unroll
             for (int i = 0; i < 2; i++) {
-                uint32_t ks[2 * G], km[G / 2];
+                uint32_t ks[2 * G];
                 lds_read(ks, stage + S::table(i, 0) + q * 8 * G);
-                lds_read(km, stage + S::table(i, 1) + (lane & 15) * 2 * G);
                 Kv4Op mm;
-                mm.w[0] = mm.w[2] = km[0];
-                mm.w[1] = mm.w[3] = G == 4 ? km[G / 2 - 1] : 0;
+                if (PARTS) mm.v = *(const f16x8_t *)(op + O::KM + i * 1024 + lane * 16);
+                else {
+                    uint32_t km[G / 2];
+                    lds_read(km, stage + S::table(i, 1) + (lane & 15) * 2 * G);
+                    mm.w[0] = mm.w[2] = km[0];
+                    mm.w[1] = mm.w[3] = G == 4 ? km[G / 2 - 1] : 0;
+                }
                 const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int n = 0; n < NC; n++) z[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(mm.v, x[n].sum.v, zero, 0, 0, 0);
@@ -1160,10 +1193,11 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_many_kernel(const Kv4Attn a
 #pragma unroll
     for (int n = 0; n < NC; n++) {
         const float total = quads_sum(l[n]);
-        // the groups' minima stand in the lanes of the first four rows
+        // the groups' minima: first parts in the lanes of rows 0 .. G - 1, second in those of rows G .. 2 G - 1
 #pragma unroll
         for (int g = 0; g < G; g++) {
-            const float v = __shfl(om[n][g], lane & 15);
+            float v = __shfl(om[n][g], lane & 15);
+            v += G == 4 ? __shfl(om[n][g], 16 + (lane & 15)) : __shfl(om[n][(g + 2) & 3], lane & 15);
 #pragma unroll
             for (int j = 2 * g; j < 2 * g + 2; j++)
 #pragma unroll
