@@ -244,13 +244,13 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(const Kv4View c, T *k, lo
 // ---- attention ----------------------------------------------------------------------------------
 //
 // A wave takes 16 NC columns, a column being one row and query head of a sequence and cache head, over steps of 32 tokens (two tiles of 16).
-//   scores   z[t][c] = f_c (sum_g s_tg (n_t . q_c)_g + m_tg . (sum of q_c)_g): the levels n are exact in fp16, so a group's 32 products are one
+//   scores   z[t][c] = f_c (sum_g s_tg ((n_t - 8) . q_c)_g + (m_tg + 8 s_tg) (sum of q_c)_g): the levels are exact in fp16, so a group's 32 products are one
 //            matrix instruction for each of two fp16 parts of the query (scaled by a power of two to below 2^10: the parts hold 24
-//            bits), its scale a multiplication in fp32; the minima are one more instruction over the groups, whose result the others add to.
+//            bits), its scale a multiplication in fp32.  (Counted from the eighth, the sums that nearly cancel are half as large as from the first.)
 //   softmax  over steps with a running reference M_c, the largest z_t + e_t seen, where the token's value scales are below 2^(e_t - 14):
 //            2^(z - M + 28) s is then below 2^14 whatever the sizes of values and scales, and as two fp16 parts is held to 24 bits
 //            and 2^-39 of the largest.
-//   values   o[d][c] = sum_t n_td (p_t s_tg)_c as matrix instructions, the levels again exact; sum_t p_t m_tg in fp32.
+//   values   o[d][c] = sum_t (n_td - 8) (p_t s_tg)_c as matrix instructions, the levels again exact; sum_t p_t (m_tg + 8 s_tg) in fp32.
 // The scores of a lane (column lane % 16, tokens 4 (lane / 16) + 0..3 of both tiles) are the products' side of the second matrix
 // instruction, so probabilities never leave the lane.
 struct Kv4Attn {
@@ -364,6 +364,7 @@ template <int CB> __device__ __forceinline__ Kv4Cols kv4_columns(const Kv4Attn &
 // One column tile's queries: the products' side of the score instructions.  LO: the second part; 16-bit queries are exact without.
 template <int D, bool LO> struct Kv4Query {
     Kv4Op hi[D / 32], lo[LO ? D / 32 : 1], sum;      // slot 2 i, 2 i + 1 of lane group q: components 8 q + i, 8 q + i + 4 of the group
+    float total[4];                         // the groups' sums of the queries, scaled as the parts
     float f;                                // what a sum of products is worth as a base-2 exponent: not negative, the scale's sign is in the parts
 
     // CENTRE: the first parts of the sums in lane group 1 too, against the second parts of m + 8 s (Kv4Ops)
@@ -384,7 +385,7 @@ template <int D, bool LO> struct Kv4Query {
         f = fmaxf(__builtin_amdgcn_ldexpf(fabsf(scale) * 1.44269504088896341f, ex - 10), 1.17549435e-38f);     // (above 0: a masked score stays -inf)
         const float sign = scale < 0.f ? -1.f : 1.f;
         uint32_t sh[2] = {0, 0}, sl[2] = {0, 0};
-        float total[4] = {0.f, 0.f, 0.f, 0.f};
+        total[0] = total[1] = total[2] = total[3] = 0.f;
 #pragma unroll
         for (int g = 0; g < G; g++) {
             float t = 0.f;
@@ -464,12 +465,12 @@ template <int D> struct Kv4Keys {
         __builtin_memcpy(m, __builtin_assume_aligned(stage + Kv4Stage<D>::table(i, 1) + tok * 2 * G, 2 * G), 2 * G);
     }
     // the levels as the other side of the score instructions
-    __device__ __forceinline__ void widen(f16x8_t (&k)[G]) const
+    template <int CENTRE = 0> __device__ __forceinline__ void widen(f16x8_t (&k)[G]) const
     {
 #pragma unroll
         for (int g = 0; g < G; g++) {
             Kv4Op o;
-            kv4_widen(w[g], o.w);
+            kv4_widen<CENTRE>(w[g], o.w);
             k[g] = o.v;
         }
     }
@@ -549,8 +550,8 @@ template <int D, int NV> struct Kv4Few {
     // One step of 32 tokens from t0 on, its numbers in LDS.  MASK: lim[i] is the number of tokens that the lane's columns see, here: the tiles that
     // have a page.  Written so that few of the step's numbers are in registers at a time.
     template <bool MASK, bool LO>
-    __device__ __forceinline__ void step(const Kv4Query<D, LO> &x, const float (&f)[NV], const char *stage, char *xchg, const int (&lim)[NV], int here,
-                                         int t0, int lane)
+    __device__ __forceinline__ void step(const Kv4Query<D, LO> &x, const float (&qs)[NV][G], const float (&f)[NV], const char *stage, char *xchg,
+                                         const int (&lim)[NV], int here, int t0, int lane)
     {
 #pragma clang fp contract(off)                      // (all instances round alike: a row's bits do not depend on which one it went through)
         typedef Kv4Stage<D> S;
@@ -564,25 +565,18 @@ template <int D, int NV> struct Kv4Few {
             Kv4Keys<D> k;
             k.load(stage, i, lane);
             f16x8_t kk[G];
-            k.widen(kk);
-            Kv4Op mm;
-            mm.w[0] = mm.w[2] = k.m[0];
-            mm.w[1] = mm.w[3] = G == 4 ? k.m[G / 2 - 1] : 0;
+            k.template widen<8>(kk);
             const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
-            const f32x4_t zm = __builtin_amdgcn_mfma_f32_16x16x32_f16(x.sum.v, mm.v, zero, 0, 0, 0);
             float y[NV];
-#pragma unroll
-            for (int n = 0; n < NV; n++) y[n] = zm[n];
 #pragma unroll
             for (int g = 0; g < G; g++) {
                 f32x4_t d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x.hi[g].v, kk[g], zero, 0, 0, 0);
                 if (LO) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x.lo[LO ? g : 0].v, kk[g], d, 0, 0, 0);
-                const float s = number(i, 0, g);
+                const float s = number(i, 0, g), mid = fmaf(s, 8.f, half_of(k.m[g >> 1], g & 1));
 #pragma unroll
-                for (int n = 0; n < NV; n++) y[n] = fmaf(s, d[n], y[n]);
+                for (int n = 0; n < NV; n++) y[n] = fmaf(s, d[n], g == 0 ? mid * qs[n][0] : fmaf(mid, qs[n][g], y[n]));
                 whole_until(y[NV - 1], d);
             }
-            whole_until(y[NV - 1], zm);
 #pragma unroll
             for (int n = 0; n < NV; n++) z[i][n] = y[n] * f[n];
         }
@@ -647,7 +641,7 @@ template <int D, int NV> struct Kv4Few {
         }
 #pragma unroll
         for (int g = 0; g < G; g++) {
-            const float m0 = number(0, 3, g), m1 = number(1, 3, g);
+            const float m0 = fmaf(vs[0][g], 8.f, number(0, 3, g)), m1 = fmaf(vs[1][g], 8.f, number(1, 3, g));
 #pragma unroll
             for (int n = 0; n < NV; n++) {
                 const float y0 = fmaf(p[0][n], m0, om[n][g]);
@@ -666,8 +660,8 @@ template <int D, int NV> struct Kv4Few {
 #pragma unroll
             for (int a = 0; a < 2; a++) {
                 const uint32_t w0 = vw[0][2 * h + a], w1 = vw[1][2 * h + a];
-                kv4_widen((w0 & 0xffff) | w1 << 16, u[2 * a]);
-                kv4_widen(w0 >> 16 | (w1 & 0xffff0000u), u[2 * a + 1]);
+                kv4_widen<8>((w0 & 0xffff) | w1 << 16, u[2 * a]);
+                kv4_widen<8>(w0 >> 16 | (w1 & 0xffff0000u), u[2 * a + 1]);
             }
 #pragma unroll
             for (int g = 2 * h; g < 2 * h + 2; g++) {
@@ -712,8 +706,8 @@ template <int D, int NS> struct Kv4Ring {
             if (t0 + i * stride < t1) fetch(i, i, t0 + i * stride);
     }
     template <int NV, bool LO>
-    __device__ __forceinline__ void run(Kv4Few<D, NV> &state, const Kv4Query<D, LO> &x, const float (&f)[NV], char *xchg, const int (&lim)[NV], int least,
-                                        int t0)
+    __device__ __forceinline__ void run(Kv4Few<D, NV> &state, const Kv4Query<D, LO> &x, const float (&qs)[NV][D / 32], const float (&f)[NV], char *xchg,
+                                        const int (&lim)[NV], int least, int t0)
     {
         int slot = 0;
         for (int t = t0; t < t1; t += stride) {
@@ -724,8 +718,8 @@ template <int D, int NS> struct Kv4Ring {
             } else if (NS > 2 && t + (NS - 2) * stride < t1) loads_left<(NS - 2) * S>();
             else loads_left<0>();
             const char *stage = lds + slot * B;
-            if (t + 32 <= least && (here & 3) == 3) state.template step<false, LO>(x, f, stage, xchg, lim, here, t, lane);
-            else state.template step<true, LO>(x, f, stage, xchg, lim, here, t, lane);
+            if (t + 32 <= least && (here & 3) == 3) state.template step<false, LO>(x, qs, f, stage, xchg, lim, here, t, lane);
+            else state.template step<true, LO>(x, qs, f, stage, xchg, lim, here, t, lane);
             here >>= 2;
             slot = slot == NS - 1 ? 0 : slot + 1;
         }
@@ -788,16 +782,18 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_few_kernel(const Kv4Attn a)
     Kv4Query<D, LO> x;
     x.load((const T *)a.q + (size_t)col.row * a.q_stride + (size_t)col.head * D, live, kv4_aligned<T>(a.q, a.q_stride, 8), a.scale, q);
     // a lane's scores are of columns q, q + 4, ..: rows 4 q, 4 q + 1, ..
-    float f[NV];
+    float f[NV], qs[NV][G];
     int lim[NV];
 #pragma unroll
     for (int n = 0; n < NV; n++) {
+#pragma unroll
+        for (int g = 0; g < G; g++) qs[n][g] = __shfl(x.total[g], 4 * q + n);
         f[n] = __shfl(x.f, 4 * q + n);
         lim[n] = __shfl(live ? col.lim : 0, 4 * q + n);
     }
     Kv4Few<D, NV> state;
     state.clear();
-    steps.run(state, x, f, xchg + wave * XCHG, lim, least, t0 + 32 * wave);
+    steps.run(state, x, qs, f, xchg + wave * XCHG, lim, least, t0 + 32 * wave);
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < NV; n++) {
