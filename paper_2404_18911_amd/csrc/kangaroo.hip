@@ -2598,7 +2598,7 @@ static bool kv4_attn_shape_ok(const kg_kv4_cache *c, int n_rows, int n_heads, in
            max_len <= (1 << 30) && (size_t)n_rows * n_heads < (size_t)1 << 31;
 }
 
-// How the attention is cut.  Few columns (at most 16 a sequence on average): one workgroup of four waves per cache head, 16 columns and chunk
+// How the attention is cut.  Few columns (at most 16 a sequence on average): one workgroup of four waves per cache head, up to 16 columns and chunk
 // of the tokens.  The chunks follow from the arguments that do not change with the rows, so that a row's sums are cut alike whatever
 // stands beside it.
 struct Kv4Plan { bool few; int nv, blocks, chunk, n_chunks; };      // nv: few columns, 4 nv of them a workgroup
@@ -2609,7 +2609,7 @@ static Kv4Plan kv4_plan(const kg_kv4_cache *c, int n_rows, int n_heads, int max_
     const long cols = (long)n_rows * group;
     const int len = (int)std::min<long>(max_len, (long)c->max_pages * c->page_tokens);
     p.few = cols <= 16L * c->n_seqs;
-    // (what a wave does to a step's scores grows with nv.  One row of 32 heads over 131001 tokens: 130 us with nv = 1, 158 with 16 columns for one)
+    // (what a wave does to a step's scores grows with nv.  One row of 32 heads over 131001 tokens: 130 us with nv = 1, 158 with 16 columns for one, on one card)
     p.nv = cols <= 4L * c->n_seqs ? 1 : cols <= 8L * c->n_seqs ? 2 : 4;
     const int cb = p.few ? 4 * p.nv : KV4_MANY_COLUMNS;
     // every sequence may end in a block that is not full

@@ -122,6 +122,7 @@ __device__ __forceinline__ float kv4_clamp(float x) { return fminf(fmaxf(x, -655
 __device__ __forceinline__ bool kv4_bad(float x) { return !(fabsf(x) <= 3.402823466e38f); }
 
 // One row and head per D / 8 lanes, eight components each; a workgroup takes consecutive rows of one head, whose numbers lie together.
+// Bound by the levels' arithmetic and the stores of two bytes, not by memory: 4096 bf16 rows of 32 heads (88 MB) 39 us, 2.3 TB/s.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_append_kernel(const Kv4View c, const T *k, long k_stride, const T *v, long v_stride, const int *row_start,
                                                          int n_rows)
@@ -214,6 +215,7 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(const Kv4View c, const 
 }
 
 // Keys and values of the rows, widened.  A token without a page reads as zeros.  Eight components of a row and head per lane.
+// Bound by what it writes: 4096 rows of 32 heads to fp32 (155 MB) 30 us, 5.1 TB/s.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_read_kernel(const Kv4View c, T *k, long k_stride, T *v, long v_stride, const int *row_start, int n_rows)
 {
@@ -243,7 +245,8 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(const Kv4View c, T *k, lo
 
 // ---- attention ----------------------------------------------------------------------------------
 //
-// A wave takes 16 NC columns, a column being one row and query head of a sequence and cache head, over steps of 32 tokens (two tiles of 16).
+// A column is one row and query head of a sequence and cache head.  A wave takes 4, 8 or 16 of them (few columns: decoding, verification) or 16 NC
+// (many: prompts) over steps of 32 tokens (two tiles of 16).  What both kernels compute:
 //   scores   z[t][c] = f_c (sum_g s_tg ((n_t - 8) . q_c)_g + (m_tg + 8 s_tg) (sum of q_c)_g): the levels are exact in fp16, so a group's 32 products are one
 //            matrix instruction for each of two fp16 parts of the query (scaled by a power of two to below 2^10: the parts hold 24
 //            bits), its scale a multiplication in fp32.  (Counted from the eighth, the sums that nearly cancel are half as large as from the first.)
@@ -251,8 +254,8 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(const Kv4View c, T *k, lo
 //            2^(z - M + 28) s is then below 2^14 whatever the sizes of values and scales, and as two fp16 parts is held to 24 bits
 //            and 2^-39 of the largest.
 //   values   o[d][c] = sum_t (n_td - 8) (p_t s_tg)_c as matrix instructions, the levels again exact; sum_t p_t (m_tg + 8 s_tg) in fp32.
-// The scores of a lane (column lane % 16, tokens 4 (lane / 16) + 0..3 of both tiles) are the products' side of the second matrix
-// instruction, so probabilities never leave the lane.
+// With many columns the scores of a lane (column lane % 16, tokens 4 (lane / 16) + 0..3 of both tiles) are the products' side of the second
+// matrix instruction, so probabilities never leave the lane, and the softmax and the values' operands are as said there.
 struct Kv4Attn {
     Kv4View c;
     const void *q;
@@ -304,7 +307,7 @@ template <int CENTRE = 0> __device__ __forceinline__ void kv4_widen(uint32_t w, 
 __device__ __forceinline__ float half_of(uint32_t w, int i) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(i ? w >> 16 : w)); }
 
 // A pair of numbers as halves (one instruction), and in two parts, of which the second takes what the first leaves: 2^-24 of the number at
-// most are lost.  (Parts rounded towards zero lose up to 2^-21, all to one side: outputs over 131001 tokens were off by 7.2e-6 instead of 2.1e-6.)
+// most are lost.  (Parts rounded towards zero lose up to 2^-21, all to one side: outputs over 131001 tokens were off by 7.2e-6 instead of 2.1e-6, with levels counted from the first.)
 __device__ __forceinline__ uint32_t kv4_halves(float x, float y) { return __builtin_bit_cast(uint32_t, f16x2_t{(_Float16)x, (_Float16)y}); }
 __device__ __forceinline__ void kv4_split(float x, float y, uint32_t &hi, uint32_t &lo)
 {
@@ -529,7 +532,9 @@ __device__ __forceinline__ void whole_until(float &y, const f32x4_t &d) { asm(""
 // with one or four columns no lane computes an exponential or splits a product for a column that is not there.  The probabilities
 // times the values' scales go through LDS (xchg) to the lanes that multiply them: products 2 j, 2 j + 1 of lane group q are tokens 4 q + j of
 // both tiles.
-//   One row of 32 heads over 131001 tokens (671 MB): 130 us, 5.2 TB/s (a plain read of memory: 6.5); 158 where every lane held 16 columns.
+//   Bound by memory where the cache is long: one row of 32 heads over 131001 tokens (671 MB) 130 to 146 us by the card, 5.2 to 4.6 TB/s (a plain read
+//   of memory: 6.5); 158 us against the 130 where every lane held 16 columns.  Levels counted from the eighth cost 2 % of that and leave
+//   8.8e-7 of error for 2.1e-6.  Short caches are a chain of latencies: 500 tokens 6.2 us of which 0.5 is memory.
 template <int D, int NV> struct Kv4Few {
     static constexpr int G = D / 32, DT = D / 16, VH = D / 64, C = 4 * NV;
     static constexpr int XCHG = G * 2 * C * 64;         // bytes: [group][part][column][16 tokens] pairs of halves
@@ -848,6 +853,9 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_few_kernel(const Kv4Attn a)
 //     half of the matrix instructions and of what is read from LDS.
 // Steps with a scale of 2048 or a minimum of 16384 or more take a sixteenth of the values (they might not fit a half) and 16 p.
 // A value scale that is not a number counts as 0 here and makes the outputs of the columns that see it NaN (nan).
+//   2048 bf16 rows of 32 heads behind 4096 tokens (172 GFLOP): 461 us, 373 TFLOP/s, a third of a large library product.  A step's matrix
+//   instructions (154 us in all) and vector instructions (218 us) follow one another at two waves a SIMD; tiles of 16 or 64 columns a wave,
+//   rings of two or four steps and three waves a SIMD (which spill) were no faster.
 template <int D> struct Kv4Ops {                // byte offsets of a step's operands, 16 bytes a lane each
     static constexpr int G = D / 32, DT = D / 16, K = 0, VHI = 2 * G * 1024, VLO = VHI + DT * 1024, VM = VLO + DT * 1024, KM = VM + 1024;
     static constexpr int bytes(bool parts) { return parts ? KM + 2 * 1024 : VLO; }
@@ -1224,6 +1232,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attend_many_kernel(const Kv4Attn a
 __device__ __forceinline__ int kv4_row_chunks(const Kv4Attn &a, int lim) { return max(1, (lim + a.chunk - 1) / a.chunk); }
 
 // Joins the chunks of a row and head, a workgroup each: wave w takes chunks w, w + 4, .., lane j of it the reference and sum of the j-th.
+// A launch's latency: 3 us for 4 chunks of 32 heads, 4.8 for 16.
 template <typename T, int D> __device__ __forceinline__ void kv4_join(const Kv4Attn &a, int item, float *lds)
 {
     float (*os)[D] = (float (*)[D])lds, *ms = lds + 4 * D, *ls = ms + 4;
@@ -1289,7 +1298,9 @@ __device__ __forceinline__ float kv4_lse(const Kv4Attn &a, size_t item, int lim,
 // What follows the chunks of a call with weights, in one launch: workgroups below n_join join a row and head (none where there is one chunk);
 // the others take 128 tokens of a sequence and cache head, 32 a wave, and go over all columns that see them:
 //     w_out[t] = w_in[t] + sum over the columns of 2^(z - lse), the scores those of the attention.
-// Four tiles of columns at a time are made ready in LDS, one by each wave.
+// Four tiles of columns at a time are made ready in LDS, one by each wave.  Bound by that preparation where there are few columns (7 rows of 32
+// heads, 4103 tokens 13 to 15 us; several blocks of tokens over one preparation gain a twentieth there and lose one in a hundred with prompts) and
+// by exponentials and their sums with prompts (777 and 131 rows of 40 heads 50 us).
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void kv4_weights_kernel(const Kv4Attn a, int n_join, int token_blocks)
 {
@@ -1529,7 +1540,8 @@ __global__ __launch_bounds__(1024) void kv4_select_kernel(const Kv4Evict a)
 }
 
 // The kept tokens' numbers, moved together.  Four tokens of the new page per 16 lanes: lane l carries piece l % 4 of the keys of token l / 4, the
-// values' halfwords r = l of all four, and one number of each of the four tables of scales.
+// values' halfwords r = l of all four, and one number of each of the four tables of scales.  Bound by gathering the values two bytes at a time:
+// 2048 of 4096 tokens, 32 heads (21 MB read and written) 21 us; the tables four tokens at a time instead: 22.
 template <int D>
 __global__ __launch_bounds__(256) void kv4_move_kernel(const Kv4Evict a)
 {
