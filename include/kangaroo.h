@@ -429,6 +429,8 @@ int kg_op_stream_read(const void *src_dev, size_t bytes, void *work_dev, void *h
  *                weights_out [n_seqs][n_kv_heads][dst max_pages T]: the kept tokens' weights, then zeros.
  * Calls launch on `hip_stream`, allocate nothing and do not synchronise.  Errors: KG_EINVAL, KG_ENOSPC (work_bytes too small, n_keep more than
  * dst's page table reaches), KG_EHIP.  n_rows = 0 is allowed.
+ * A launch has fewer than 2^32 threads; calls that would need more are KG_EINVAL too: n_rows head_dim / 8 of 2^32 and more in append and read,
+ * weights of n_seqs n_kv_heads max_len (rounded up to 128) of 2^31 and more.
  */
 #define KG_KV4_MAX_HEADS 1024
 #define KG_KV4_MAX_SEQS 4096

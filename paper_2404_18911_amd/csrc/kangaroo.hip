@@ -2530,6 +2530,9 @@ static bool kv4_rows_share(const void *a, long sa, const void *b, long sb, long 
     return off < wb || off + wb > st;
 }
 
+// Workgroups of 256 threads in a launch's first dimension: it is counted in threads, in 32 bits.
+constexpr size_t KV4_MAX_GROUPS = ((size_t)1 << 24) - 1;
+
 static bool bytes_share(const void *a, size_t na, const void *b, size_t nb)
 {
     return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
@@ -2564,7 +2567,9 @@ int kg_op_kv4_append(const kg_kv4_cache *c, int dtype, const void *k, long k_str
     const long w = (long)c->n_kv_heads * c->head_dim;
     if (!kv4_rows_ok(k, k_stride, w, n_rows, esz) || !kv4_rows_ok(v, v_stride, w, n_rows, esz)) return KG_EINVAL;
     const Kv4View view = kv4_view(c);
-    const dim3 grid((unsigned)(((size_t)n_rows * (c->head_dim / 8) + 255) / 256), c->n_kv_heads);
+    const size_t groups = ((size_t)n_rows * (c->head_dim / 8) + 255) / 256;
+    if (groups > KV4_MAX_GROUPS) return KG_EINVAL;
+    const dim3 grid((unsigned)groups, c->n_kv_heads);
 #define KV4_LAUNCH(T, D) \
     hipLaunchKernelGGL((kv4_append_kernel<T, D>), grid, dim3(256), 0, (hipStream_t)hip_stream, view, (const T *)k, k_stride, (const T *)v, v_stride, row_start, n_rows)
     KV4_BY_TYPE_AND_DIM(KV4_LAUNCH, c->head_dim);
@@ -2582,7 +2587,9 @@ int kg_op_kv4_read(const kg_kv4_cache *c, int dtype, void *k, long k_stride, voi
     if (!kv4_rows_ok(k, k_stride, w, n_rows, esz) || !kv4_rows_ok(v, v_stride, w, n_rows, esz)) return KG_EINVAL;
     if (kv4_rows_share(k, k_stride, v, v_stride, w, n_rows, esz)) return KG_EINVAL;
     const Kv4View view = kv4_view(c);
-    const dim3 grid((unsigned)(((size_t)n_rows * (c->head_dim / 8) + 255) / 256), c->n_kv_heads);
+    const size_t groups = ((size_t)n_rows * (c->head_dim / 8) + 255) / 256;
+    if (groups > KV4_MAX_GROUPS) return KG_EINVAL;
+    const dim3 grid((unsigned)groups, c->n_kv_heads);
 #define KV4_LAUNCH(T, D) \
     hipLaunchKernelGGL((kv4_read_kernel<T, D>), grid, dim3(256), 0, (hipStream_t)hip_stream, view, (T *)k, k_stride, (T *)v, v_stride, row_start, n_rows)
     KV4_BY_TYPE_AND_DIM(KV4_LAUNCH, c->head_dim);
@@ -2649,19 +2656,19 @@ int kg_op_kv4_attention(const kg_kv4_cache *c, int dtype, const void *q, long q_
     const size_t cap = (size_t)c->max_pages * c->page_tokens, w_bytes = (size_t)c->n_seqs * c->n_kv_heads * cap * 4;
     if (weights_in && weights_in != weights_out && bytes_share(weights_in, w_bytes, weights_out, w_bytes)) return KG_EINVAL;
     if (n_rows == 0 && !weights_out) return KG_OK;
-    if ((size_t)n_rows * n_heads + ((size_t)std::min<size_t>(max_len, cap) / 128 + 1) * c->n_kv_heads * c->n_seqs >= (size_t)1 << 31) return KG_EINVAL;
+    const Kv4Plan p = n_rows > 0 ? kv4_plan(c, n_rows, n_heads, max_len) : Kv4Plan{false, 1, 0, 0, 1};
+    const size_t lanes = (size_t)n_rows * n_heads, joins = p.n_chunks > 1 ? lanes : 0;
+    const size_t token_blocks = (std::min<size_t>(max_len, cap) + 127) / 128, blocks = weights_out ? token_blocks * c->n_kv_heads * c->n_seqs : 0;
+    if ((size_t)p.blocks > KV4_MAX_GROUPS || joins + blocks > KV4_MAX_GROUPS) return KG_EINVAL;
     Kv4Attn a;
     memset(&a, 0, sizeof(a));
     a.c = kv4_view(c); a.q = q; a.out = out; a.q_stride = q_stride; a.out_stride = out_stride; a.row_start = row_start; a.n_rows = n_rows;
     a.heads = n_heads; a.group = n_heads / c->n_kv_heads; a.max_len = (int)std::min<size_t>(max_len, cap); a.scale = scale;
     a.w_in = weights_in; a.w_out = weights_out; a.lse = (float *)work;
     hipStream_t s = (hipStream_t)hip_stream;
-    Kv4Plan p = {};
-    const size_t lanes = (size_t)n_rows * n_heads;
-    a.n_chunks = 1;
+    a.n_chunks = p.n_chunks;
     if (n_rows > 0) {
-        p = kv4_plan(c, n_rows, n_heads, max_len);
-        a.chunk = p.chunk; a.n_chunks = p.n_chunks; a.shift = p.few ? KV4_SHIFT : KV4_MANY_SHIFT;
+        a.chunk = p.chunk; a.shift = p.few ? KV4_SHIFT : KV4_MANY_SHIFT;
         a.part_ml = (float2 *)((char *)work + up(lanes * 4));
         a.part = (float *)((char *)a.part_ml + up(lanes * p.n_chunks * 8));
         const dim3 grid(p.blocks, c->n_kv_heads, p.n_chunks);
@@ -2682,9 +2689,8 @@ int kg_op_kv4_attention(const kg_kv4_cache *c, int dtype, const void *q, long q_
 #undef KV4_JOIN
     }
     if (weights_out) {
-        const int n_join = a.n_chunks > 1 ? (int)lanes : 0, token_blocks = (a.max_len + 127) / 128;
-        const dim3 wgrid((unsigned)(n_join + (size_t)token_blocks * c->n_kv_heads * c->n_seqs));
-#define KV4_LAUNCH(T, D) hipLaunchKernelGGL((kv4_weights_kernel<T, D>), wgrid, dim3(256), 0, s, a, n_join, token_blocks)
+        const dim3 wgrid((unsigned)(joins + blocks));
+#define KV4_LAUNCH(T, D) hipLaunchKernelGGL((kv4_weights_kernel<T, D>), wgrid, dim3(256), 0, s, a, (int)joins, (int)token_blocks)
         KV4_BY_TYPE_AND_DIM(KV4_LAUNCH, c->head_dim);
 #undef KV4_LAUNCH
     }

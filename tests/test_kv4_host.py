@@ -142,3 +142,17 @@ def test_oracle_eviction_by_hand():
     assert list(O.evict(w, 4, 5, 1, 2)) == [0, 1, 2, 3]
     w[4] = np.nan
     assert list(O.evict(w, 10, 4, 0, 0)) == [0, 2, 4, 7]
+
+
+@pytest.mark.parametrize("head_dim", [64, 128])
+def test_calls_beyond_a_launch_are_refused(head_dim):
+    """A launch has fewer than 2^32 threads: such a call is an error of its arguments, found before anything runs."""
+    L, p, far = B.lib(), 1 << 20, 1 << 46
+    c, n = _cache(head_dim=head_dim), (1 << 32) * 8 // head_dim      # head_dim / 8 threads a row and head
+    w = 4 * head_dim
+    assert L.kg_op_kv4_append(c, 1, p, w, far, w, p, n, None) == B.KG_EINVAL
+    assert L.kg_op_kv4_read(c, 1, p, w, far, w, p, n, None) == B.KG_EINVAL
+    # weights: 256 threads for 128 tokens of a sequence and head, 2^24 such blocks
+    c = _cache(head_dim=head_dim, n_kv_heads=1024, n_seqs=16, max_pages=1 << 11, page_stride=1024 * 64 * head_dim * 5 // 4)
+    work = L.kg_op_kv4_work_bytes(c, 0, 1024, 1 << 17)
+    assert L.kg_op_kv4_attention(c, 0, None, 0, 1024, p, 0, 1 << 17, 0.1, None, 0, None, far, p, work, None) == B.KG_EINVAL
