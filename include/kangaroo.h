@@ -427,6 +427,7 @@ int kg_op_stream_read(const void *src_dev, size_t bytes, void *work_dev, void *h
  *                (other pages than src's, which are only read; dst's len_dev is not read: the caller sets it to min(len, n_keep)).
  *                kept [n_seqs][n_kv_heads][n_keep]: which tokens, -1 behind a sequence that is not that long (it is copied whole).
  *                weights_out [n_seqs][n_kv_heads][dst max_pages T]: the kept tokens' weights, then zeros.
+ *                weights_in, weights_out and kept must not overlap.
  * Calls launch on `hip_stream`, allocate nothing and do not synchronise.  Errors: KG_EINVAL, KG_ENOSPC (work_bytes too small, n_keep more than
  * dst's page table reaches), KG_EHIP.  n_rows = 0 is allowed.
  * A launch has fewer than 2^32 threads; calls that would need more are KG_EINVAL too: n_rows head_dim / 8 of 2^32 and more in append and read,

@@ -2707,6 +2707,8 @@ int kg_op_kv4_evict(const kg_kv4_cache *src, const kg_kv4_cache *dst, int n_keep
     if ((size_t)n_keep > out_cap) return KG_ENOSPC;
     const size_t heads = (size_t)src->n_seqs * src->n_kv_heads;
     if (bytes_share(weights_in, heads * in_cap * 4, weights_out, heads * out_cap * 4)) return KG_EINVAL;
+    const size_t kept_bytes = heads * n_keep * 4;
+    if (bytes_share(kept, kept_bytes, weights_in, heads * in_cap * 4) || bytes_share(kept, kept_bytes, weights_out, heads * out_cap * 4)) return KG_EINVAL;
     Kv4Evict a;
     a.src = kv4_view(src); a.dst = kv4_view(dst); a.keep = n_keep; a.first = n_first; a.recent = n_recent;
     a.w_in = weights_in; a.w_out = weights_out; a.kept = kept;

@@ -156,3 +156,9 @@ def test_calls_beyond_a_launch_are_refused(head_dim):
     c = _cache(head_dim=head_dim, n_kv_heads=1024, n_seqs=16, max_pages=1 << 11, page_stride=1024 * 64 * head_dim * 5 // 4)
     work = L.kg_op_kv4_work_bytes(c, 0, 1024, 1 << 17)
     assert L.kg_op_kv4_attention(c, 0, None, 0, 1024, p, 0, 1 << 17, 0.1, None, 0, None, far, p, work, None) == B.KG_EINVAL
+
+
+@pytest.mark.parametrize("kept", [(1 << 20) + 64, (1 << 21) + 64])
+def test_evict_refuses_kept_tokens_over_the_weights(kept):
+    L, src, dst, p = B.lib(), _cache(), _cache(max_pages=2), 1 << 20
+    assert L.kg_op_kv4_evict(src, dst, 100, 4, 32, p, 2 * p, kept, None) == B.KG_EINVAL
