@@ -411,7 +411,7 @@ template <int D, bool LO> struct Kv4Query {
 // A step's numbers in LDS, brought there without passing registers (lds_load16: 16 bytes a lane, lane after lane, from any addresses):
 // keys of both tiles as their readers want them, values likewise, then for each tile its parts of the four tables.
 template <int D> struct Kv4Stage {
-    static constexpr int G = D / 32, BYTES = D == 128 ? 5120 : 3072, LOADS = D == 128 ? 5 : 3;
+    static constexpr int G = D / 32, LOADS = D == 128 ? 5 : 3, BYTES = LOADS * 1024;
     static __device__ __forceinline__ int k_read(int i, int lane)
     {
         return D == 128 ? i * 1024 + lane * 16 : i * 512 + ((lane & 15) + (lane >> 5) * 16) * 16 + (lane >> 4 & 1) * 8;
